@@ -129,7 +129,8 @@ typedef enum {
                         message behind the compression rate quoted in Section 5.2 */
 } bpc_kind_t;
 
-typedef enum { BPC_F32 = 0, BPC_F16 = 1 } bpc_dtype_t;
+/* Gradients are F32 or F16; logits may be BF16 too. */
+typedef enum { BPC_F32 = 0, BPC_F16 = 1, BPC_BF16 = 2 } bpc_dtype_t;
 typedef enum { BPC_NORM_L2 = 0, BPC_NORM_LINF = 1 } bpc_norm_t;
 typedef enum {
   BPC_OPT_LANS = 0, /* Algorithm 5 as printed (block-normalised update) */
@@ -340,6 +341,131 @@ bpc_status_t bpc_adaptive_update(const bpc_params_t *params,
                                  const void *payload, uint64_t D, float *param,
                                  float *m, float *v, const bpc_opt_t *opt,
                                  void *ws, size_t ws_bytes, void *hip_stream);
+
+/*
+ * Distillation from a teacher's top logits
+ * ----------------------------------------
+ * Teachers send students the k largest logits of every row (token, image) as a
+ * top-k message instead of the whole row: bpc_logits_topk() makes the messages,
+ * bpc_distill_loss(), bpc_distill_grad() and bpc_distill_step() are the
+ * student's loss against them and its gradient with respect to the student's
+ * logits.
+ *
+ * Logits are rows of `vocab` elements of `dtype` (F32, F16, BF16), row r at
+ * element r * row_stride of a 16-byte aligned buffer; row_stride >= vocab is any
+ * number, so rows need not be aligned.  Elements between rows are never written.
+ *
+ * A message is one record per row, record r at byte r * bpc_logits_stride():
+ *   TOPK    u32 n; f32 rest; f32 top; u32 zero;  i32 idx[ru4(k)]; f32 val[ru4(k)]
+ *   TOPK16  u32 n; f32 rest; f32 top; u32 zero;  i32 idx[ru4(k)]; u16 val[2*ru4(ceil(k/2))]
+ *     n <= k   entries listed: the k largest logits of the row, ties to the lowest
+ *              index, a NaN above +inf; -inf (a masked logit) is never listed
+ *     top      the row's largest logit (-inf where n = 0)
+ *     idx      strictly ascending; -1 from n to k
+ *     val      logit - top (TOPK16: as IEEE binary16, round to nearest even); -inf
+ *              from n to k
+ *     rest     sum over the logits not listed of exp((logit - top) / temperature)
+ *   Bytes of a record past these fields are unspecified.  The student's calls read
+ *   n, rest, idx and val; whatever a record says, they read and write inside
+ *   their buffers (n is cut to k, entries with idx outside the vocabulary are
+ *   skipped; an index that is listed twice gives an unspecified result for its row).
+ *
+ * With student logits s, c = 1 / temperature, p = softmax(s c), S the listed indices,
+ * e_i = exp(val_i c), Q = sum_S e_i (TAIL_DROP) or sum_S e_i + rest (TAIL_REST),
+ * q_i = e_i / Q, q_R = rest / Q, p_R = the sum of p outside S:
+ *   KL_r   = sum_S q_i log(q_i / p_i)                        (+ q_R log(q_R / p_R) with TAIL_REST)
+ *   CE_r   = -log softmax(s)[label_r]                         (at temperature 1)
+ *   loss_r = row_weight_r * (soft_weight * KL_r + hard_weight * CE_r)
+ *   d loss_r / d s_j = row_weight_r * (soft_weight c (p_j - q_j) + hard_weight (softmax(s)_j - [j = label_r]))
+ *            where for j outside S  q_j = q_R p_j / p_R with TAIL_REST, 0 with TAIL_DROP.
+ *   (The usual soft weight is alpha * temperature^2.)
+ *   - TAIL_DROP renormalises the teacher over its listed words; TAIL_REST compares
+ *     the mass of all others as one more word.
+ *   - A row of row_weight 0 has loss 0 and a gradient of zeros, its logits are not read.
+ *   - A record with n = 0 gives no soft term, a label outside [0, vocab) (or labels
+ *     NULL, or hard_weight 0) no hard term.
+ *   - Masked student logits (-inf) have probability and gradient 0; if the teacher
+ *     gives such a word (or, with TAIL_REST, a rest that is masked as a whole) mass,
+ *     the loss is +inf and the gradient of the listed words still -q_i.
+ *   - A NaN or +inf among a row's logits makes that row's loss and gradient NaN.
+ * Unlike the gradient path these calls take infinities and NaN as described.  Sums are
+ * formed in f32 in a fixed order: the same inputs give the same bits.
+ * Limits (BPC_ERR_UNSUPPORTED beyond): vocab <= 2^24, k <= BPC_LOGITS_MAX_K (k may exceed
+ * vocab), rows < 2^22.  rows == 0 is a no-op returning BPC_OK.
+ */
+#define BPC_LOGITS_MAX_K 1024
+#define BPC_DISTILL_STATS_BYTES 32
+typedef enum { BPC_TAIL_DROP = 0, BPC_TAIL_REST = 1 } bpc_tail_t;
+typedef struct bpc_distill {
+  int32_t kind;        /* BPC_TOPK: f32 values in the messages, BPC_TOPK16: half */
+  int32_t tail;        /* bpc_tail_t */
+  uint32_t vocab;      /* logits per row */
+  uint32_t k;          /* entries a record has room for */
+  float temperature;   /* 1e-30 .. 1e30 */
+  float soft_weight, hard_weight;
+  uint32_t reserved;
+} bpc_distill_t;
+
+/* Byte stride between the records of a message; 0 on invalid arguments. */
+size_t bpc_logits_stride(const bpc_distill_t *d);
+
+/* Bytes of the messages of `rows` rows; 0 on invalid arguments or rows == 0. */
+size_t bpc_logits_message_bytes(const bpc_distill_t *d, uint64_t rows);
+
+/* Bytes of device workspace that any of the calls below may need for up to `rows`
+ * rows of any type (at least 256); 0 on invalid arguments or beyond the limits. */
+size_t bpc_distill_workspace_bytes(const bpc_distill_t *d, uint64_t rows);
+
+/*
+ * Teacher: the message of `rows` rows of logits.
+ *   row_weight  device, f32 per row, or NULL.  Rows of weight 0 are not read and get
+ *               the empty record (n = 0, rest = 0, top = -inf).
+ *   messages    device, bpc_logits_message_bytes() bytes, written
+ *   ws          device workspace of ws_bytes >= bpc_distill_workspace_bytes(d, rows)
+ */
+bpc_status_t bpc_logits_topk(const bpc_distill_t *d, const void *logits, bpc_dtype_t dtype,
+                             uint64_t row_stride, uint64_t rows, const float *row_weight,
+                             void *messages, void *ws, size_t ws_bytes, void *hip_stream);
+
+/*
+ * Student: loss of each row.
+ *   labels      device, i64 per row, or NULL
+ *   row_weight  device, f32 per row, or NULL (all 1)
+ *   loss        device, f32 per row, written
+ *   stats       device, BPC_DISTILL_STATS_BYTES per row, written, or NULL: what
+ *               bpc_distill_grad() of the same rows needs (contents unspecified)
+ */
+bpc_status_t bpc_distill_loss(const bpc_distill_t *d, const void *logits, bpc_dtype_t dtype,
+                              uint64_t row_stride, uint64_t rows, const void *messages,
+                              const int64_t *labels, const float *row_weight, float *loss,
+                              void *stats, void *ws, size_t ws_bytes, void *hip_stream);
+
+/*
+ * Student: gradient of the sum of the losses with respect to the logits, from the
+ * statistics that bpc_distill_loss() left for the same logits, messages and labels.
+ *   row_weight  as above; to carry on a gradient g_r of loss_r, pass row_weight_r * g_r.
+ *               A row whose weight was 0 in bpc_distill_loss() has no statistics: its
+ *               weight must be 0 here too.  soft_weight and hard_weight may differ from
+ *               those of bpc_distill_loss(), except that a hard_weight that was 0 there
+ *               must be 0 here; everything else in `d` must be the same.
+ *   grad        device, `rows` rows of `vocab` elements of `dtype`, row r at element
+ *               r * grad_stride, written; may be the logits themselves
+ *               (grad == logits and grad_stride == row_stride), otherwise must not overlap them
+ */
+bpc_status_t bpc_distill_grad(const bpc_distill_t *d, const void *logits, bpc_dtype_t dtype,
+                              uint64_t row_stride, uint64_t rows, const void *messages,
+                              const int64_t *labels, const float *row_weight, const void *stats,
+                              void *grad, uint64_t grad_stride, void *hip_stream);
+
+/*
+ * Student: loss and gradient in one call; the logits are read once where a workgroup
+ * can hold a row.  Arguments as above.
+ */
+bpc_status_t bpc_distill_step(const bpc_distill_t *d, const void *logits, bpc_dtype_t dtype,
+                              uint64_t row_stride, uint64_t rows, const void *messages,
+                              const int64_t *labels, const float *row_weight, float *loss,
+                              void *grad, uint64_t grad_stride, void *ws, size_t ws_bytes,
+                              void *hip_stream);
 
 /*
  * Measurement aid: a plain streaming kernel with the memory traffic of a stage and

@@ -18,17 +18,21 @@ LIB_PATH = os.path.join(_HERE, "libbpc.so")
 
 # enums of include/bpc.h
 IDENTITY, SIGN, TOPK, RANDK, DITHER, NATDITHER, FP16, TOPK16 = 0, 1, 2, 3, 4, 5, 6, 7
-F32, F16 = 0, 1
+F32, F16, BF16 = 0, 1, 2
 NORM_L2, NORM_LINF = 0, 1
 OPT_LANS, OPT_ADAM = 0, 1
+TAIL_DROP, TAIL_REST = 0, 1
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_ALIGNMENT, ERR_HIP, ERR_WAIT = range(7)
 MAX_WORKERS = 64
+LOGITS_MAX_K, DISTILL_STATS_BYTES = 1024, 32
 
 HIPCC_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-ffp-contract=off",
                "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-fPIC"]
 
 EXPORTS = ["bpc_partition_k", "bpc_partition_stride", "bpc_payload_bytes", "bpc_partition_offset", "bpc_workspace_bytes",
            "bpc_update_workspace_bytes", "bpc_workspace_status_offset", "bpc_workspace_check", "bpc_compress", "bpc_compress_static_ws", "bpc_decompress", "bpc_server_aggregate", "bpc_adaptive_update",
+           "bpc_logits_stride", "bpc_logits_message_bytes", "bpc_distill_workspace_bytes", "bpc_logits_topk",
+           "bpc_distill_loss", "bpc_distill_grad", "bpc_distill_step",
            "bpc_stream_probe", "bpc_status_string", "bpc_last_hip_error"]
 
 
@@ -82,6 +86,12 @@ class Opt(C.Structure):
                 ("reserved", C.c_uint32), ("block_offsets", C.c_void_p), ("n_blocks", C.c_uint64)]
 
 
+class Distill(C.Structure):
+    _fields_ = [("kind", C.c_int32), ("tail", C.c_int32), ("vocab", C.c_uint32), ("k", C.c_uint32),
+                ("temperature", C.c_float), ("soft_weight", C.c_float), ("hard_weight", C.c_float),
+                ("reserved", C.c_uint32)]
+
+
 _lib = None
 
 
@@ -123,6 +133,21 @@ def lib():
         L.bpc_adaptive_update.argtypes = [PP, C.c_void_p, C.c_uint64, C.c_void_p, C.c_void_p, C.c_void_p,
                                           C.POINTER(Opt), C.c_void_p, C.c_size_t, C.c_void_p]
         L.bpc_adaptive_update.restype = C.c_int
+        DP, V, U = C.POINTER(Distill), C.c_void_p, C.c_uint64
+        L.bpc_logits_stride.argtypes = [DP]
+        L.bpc_logits_stride.restype = C.c_size_t
+        L.bpc_logits_message_bytes.argtypes = [DP, U]
+        L.bpc_logits_message_bytes.restype = C.c_size_t
+        L.bpc_distill_workspace_bytes.argtypes = [DP, U]
+        L.bpc_distill_workspace_bytes.restype = C.c_size_t
+        L.bpc_logits_topk.argtypes = [DP, V, C.c_int, U, U, V, V, V, C.c_size_t, V]
+        L.bpc_logits_topk.restype = C.c_int
+        L.bpc_distill_loss.argtypes = [DP, V, C.c_int, U, U, V, V, V, V, V, V, C.c_size_t, V]
+        L.bpc_distill_loss.restype = C.c_int
+        L.bpc_distill_grad.argtypes = [DP, V, C.c_int, U, U, V, V, V, V, V, U, V]
+        L.bpc_distill_grad.restype = C.c_int
+        L.bpc_distill_step.argtypes = [DP, V, C.c_int, U, U, V, V, V, V, V, U, V, C.c_size_t, V]
+        L.bpc_distill_step.restype = C.c_int
         L.bpc_stream_probe.argtypes = [C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_uint64, C.c_void_p]
         L.bpc_stream_probe.restype = C.c_int
         L.bpc_status_string.argtypes = [C.c_int]
@@ -301,3 +326,125 @@ def bpc_adaptive_update(p: Params, payload, param, m, v, opt: Opt, ws, stream=No
     st = lib().bpc_adaptive_update(C.byref(p), _ptr(payload), param.numel(), _ptr(param), _ptr(m), _ptr(v),
                                    C.byref(opt), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream))
     _check(st, "bpc_adaptive_update")
+
+
+def make_distill(kind, vocab, k, temperature=1.0, soft_weight=1.0, hard_weight=0.0, tail=TAIL_DROP) -> Distill:
+    """``kind``: TOPK or TOPK16 (values of the messages in f32 or half precision); ``tail``: TAIL_DROP
+    or TAIL_REST."""
+    d = Distill()
+    d.kind, d.tail, d.temperature = int(kind), int(tail), temperature
+    if not (0 <= vocab < 1 << 32 and 0 <= k < 1 << 32):
+        raise ValueError(f"vocab {vocab} or k {k} out of range")
+    d.vocab, d.k, d.soft_weight, d.hard_weight, d.reserved = int(vocab), int(k), soft_weight, hard_weight, 0
+    return d
+
+
+def logits_stride(d: Distill) -> int:
+    return int(lib().bpc_logits_stride(C.byref(d)))
+
+
+def logits_message_bytes(d: Distill, rows: int) -> int:
+    return int(lib().bpc_logits_message_bytes(C.byref(d), rows))
+
+
+def distill_workspace_bytes(d: Distill, rows: int) -> int:
+    return int(lib().bpc_distill_workspace_bytes(C.byref(d), rows))
+
+
+_LOGITS_DTYPES = {"torch.float32": F32, "torch.float16": F16, "torch.bfloat16": BF16}
+_logits_codes = {}
+
+
+def _logits(t, d, what):
+    """(dtype code, rows, row stride) of a GPU tensor [rows, vocab] whose rows are contiguous; the stride
+    of a single row is its length, whatever the tensor says."""
+    code = _logits_codes.get(t.dtype)
+    if code is None:
+        code = _LOGITS_DTYPES.get(str(t.dtype))
+        if code is None:
+            raise TypeError(f"{what} dtype {t.dtype} not supported")
+        _logits_codes[t.dtype] = code
+    if t.dim() != 2 or t.shape[1] != d.vocab or (d.vocab > 1 and t.stride(1) != 1):
+        raise ValueError(f"{what}: expected [rows, {d.vocab}] with contiguous rows, got {tuple(t.shape)}, strides {t.stride()}")
+    rows = t.shape[0]
+    return code, rows, (t.stride(0) if rows > 1 else d.vocab)
+
+
+def _per_row(t, dtype, rows, what, per=1, optional=True):
+    """A contiguous tensor of at least ``per`` elements a row; its pointer."""
+    if t is None:
+        if optional:
+            return None
+        raise ValueError(f"{what} missing")
+    if str(t.dtype) != dtype or t.numel() < rows * per or not t.is_contiguous():
+        raise ValueError(f"{what}: expected a contiguous {dtype} tensor of at least {rows * per} elements, got {tuple(t.shape)} {t.dtype}")
+    return t.data_ptr()
+
+
+def _same_device(*tensors):
+    """The kernels run on the current device: every tensor has to be there."""
+    global _torch
+    if _torch is None:
+        import torch
+
+        _torch = torch
+    at = _torch.cuda.current_device() if _torch.cuda.is_available() else -1
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.get_device() != at):
+            raise ValueError(f"tensor on {t.device}, the current device is cuda:{at}")
+
+
+def bpc_logits_topk(d: Distill, logits, row_weight, messages, ws, stream=None) -> None:
+    """messages = the k largest logits of every row of ``logits`` [rows, vocab] and the mass of the rest."""
+    code, rows, stride = _logits(logits, d, "logits")
+    _same_device(logits, row_weight, messages, ws)
+    st = lib().bpc_logits_topk(C.byref(d), logits.data_ptr(), code, stride, rows,
+                               _per_row(row_weight, "torch.float32", rows, "row_weight"),
+                               _per_row(messages, "torch.uint8", rows, "messages", logits_stride(d), False),
+                               _ptr(ws), ws.numel() * ws.element_size(), _stream(stream))
+    _check(st, "bpc_logits_topk")
+
+
+def _student(d, logits, messages, labels, row_weight):
+    code, rows, stride = _logits(logits, d, "logits")
+    return rows, (C.byref(d), logits.data_ptr(), code, stride, rows,
+                  _per_row(messages, "torch.uint8", rows, "messages", logits_stride(d), False),
+                  _per_row(labels, "torch.int64", rows, "labels"),
+                  _per_row(row_weight, "torch.float32", rows, "row_weight"))
+
+
+def _gradient(grad, logits, d, rows):
+    code, grows, stride = _logits(grad, d, "grad")
+    if grad.dtype != logits.dtype or grows != rows:
+        raise ValueError(f"grad: expected {tuple(logits.shape)} {logits.dtype}, got {tuple(grad.shape)} {grad.dtype}")
+    return grad.data_ptr(), stride
+
+
+def bpc_distill_loss(d: Distill, logits, messages, labels, row_weight, loss, stats, ws, stream=None) -> None:
+    """loss[r] of the student's ``logits`` [rows, vocab] against the teacher's messages (and ``labels``, or
+    None); ``stats``: uint8 [rows, 32] for bpc_distill_grad, or None."""
+    rows, args = _student(d, logits, messages, labels, row_weight)
+    _same_device(logits, messages, labels, row_weight, loss, stats, ws)
+    st = lib().bpc_distill_loss(*args, _per_row(loss, "torch.float32", rows, "loss", 1, False),
+                                _per_row(stats, "torch.uint8", rows, "stats", DISTILL_STATS_BYTES),
+                                _ptr(ws), ws.numel() * ws.element_size(), _stream(stream))
+    _check(st, "bpc_distill_loss")
+
+
+def bpc_distill_grad(d: Distill, logits, messages, labels, row_weight, stats, grad, stream=None) -> None:
+    """grad = d sum(loss) / d logits from the statistics of bpc_distill_loss; ``grad`` may be ``logits``."""
+    rows, args = _student(d, logits, messages, labels, row_weight)
+    _same_device(logits, messages, labels, row_weight, stats, grad)
+    st = lib().bpc_distill_grad(*args, _per_row(stats, "torch.uint8", rows, "stats", DISTILL_STATS_BYTES, False),
+                                *_gradient(grad, logits, d, rows), _stream(stream))
+    _check(st, "bpc_distill_grad")
+
+
+def bpc_distill_step(d: Distill, logits, messages, labels, row_weight, loss, grad, ws, stream=None) -> None:
+    """bpc_distill_loss and bpc_distill_grad in one call."""
+    rows, args = _student(d, logits, messages, labels, row_weight)
+    _same_device(logits, messages, labels, row_weight, loss, grad, ws)
+    st = lib().bpc_distill_step(*args, _per_row(loss, "torch.float32", rows, "loss", 1, False),
+                                *_gradient(grad, logits, d, rows), _ptr(ws), ws.numel() * ws.element_size(),
+                                _stream(stream))
+    _check(st, "bpc_distill_step")

@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 #include <mutex>
 #include "cluster.hpp"
+#include "distill_geometry.hpp"
 #include "kernels.hpp"
 
 using namespace bpc;
@@ -406,6 +407,118 @@ bpc_status_t bpc_adaptive_update(const bpc_params_t *params, const void *payload
     if (e != hipSuccess) return hip_status(e);
   }
   return BPC_OK;
+}
+
+size_t bpc_logits_stride(const bpc_distill_t *d) {
+  return distill_valid(d) && distill_built(d, 0) ? logits_stride(d) : 0;
+}
+
+size_t bpc_logits_message_bytes(const bpc_distill_t *d, uint64_t rows) {
+  return distill_valid(d) && distill_built(d, rows) ? (size_t)rows * logits_stride(d) : 0;
+}
+
+size_t bpc_distill_workspace_bytes(const bpc_distill_t *d, uint64_t rows) {
+  return distill_valid(d) && distill_built(d, rows) ? distill_workspace(d, rows) : 0;
+}
+
+// What the four calls have in common: their description, shape and logits.
+static bpc_status_t check_rows(const bpc_distill_t *d, const void *logits, bpc_dtype_t dtype, uint64_t row_stride, uint64_t rows) {
+  if (!distill_valid(d)) return BPC_ERR_INVALID_ARG;
+  if (dtype != BPC_F32 && dtype != BPC_F16 && dtype != BPC_BF16) return BPC_ERR_INVALID_ARG;
+  if (row_stride < d->vocab) return BPC_ERR_INVALID_ARG;
+  if (!distill_built(d, rows) || row_stride > kMaxRowStride) return BPC_ERR_UNSUPPORTED;
+  if (rows != 0 && !logits) return BPC_ERR_INVALID_ARG;
+  return aligned16(logits) ? BPC_OK : BPC_ERR_ALIGNMENT;
+}
+static DistillCall distill_call(const bpc_distill_t *d, const void *logits, bpc_dtype_t dtype, uint64_t row_stride, uint64_t rows) {
+  DistillCall c{};
+  c.logits = logits;
+  c.dtype = (int)dtype;
+  c.row_stride = row_stride;
+  c.rows = rows;
+  c.vocab = d->vocab;
+  c.k = d->k;
+  c.message_stride = logits_stride(d);
+  c.half = d->kind == BPC_TOPK16;
+  c.rest_too = d->tail == BPC_TAIL_REST;
+  c.temperature = d->temperature;
+  c.soft = d->soft_weight;
+  c.hard = d->hard_weight;
+  return c;
+}
+
+bpc_status_t bpc_logits_topk(const bpc_distill_t *d, const void *logits, bpc_dtype_t dtype, uint64_t row_stride, uint64_t rows,
+                             const float *row_weight, void *messages, void *ws, size_t ws_bytes, void *hip_stream) {
+  const bpc_status_t st = check_rows(d, logits, dtype, row_stride, rows);
+  if (st != BPC_OK) return st;
+  if (rows == 0) return BPC_OK;
+  if (!messages) return BPC_ERR_INVALID_ARG;
+  if (!aligned16(row_weight) || !aligned16(messages) || !aligned16(ws)) return BPC_ERR_ALIGNMENT;
+  if (!ws || ws_bytes < distill_workspace(d, rows)) return BPC_ERR_WORKSPACE;
+  DistillCall c = distill_call(d, logits, dtype, row_stride, rows);
+  c.weight = row_weight;
+  return hip_status(logits_topk(c, (uint8_t *)messages, (uint8_t *)ws, (hipStream_t)hip_stream));
+}
+
+// bpc_distill_loss and bpc_distill_step
+static bpc_status_t distill_forward(DistillRole role, const bpc_distill_t *d, const void *logits, bpc_dtype_t dtype,
+                                    uint64_t row_stride, uint64_t rows, const void *messages, const int64_t *labels,
+                                    const float *row_weight, float *loss, void *stats, void *grad, uint64_t grad_stride,
+                                    void *ws, size_t ws_bytes, void *hip_stream) {
+  const bpc_status_t st = check_rows(d, logits, dtype, row_stride, rows);
+  if (st != BPC_OK) return st;
+  if (role == DistillRole::step && grad_stride < d->vocab) return BPC_ERR_INVALID_ARG;
+  if (grad_stride > kMaxRowStride) return BPC_ERR_UNSUPPORTED;
+  if (rows == 0) return BPC_OK;
+  if (!messages || !loss || (role == DistillRole::step && !grad)) return BPC_ERR_INVALID_ARG;
+  if (!aligned16(messages) || !aligned16(labels) || !aligned16(row_weight) || !aligned16(loss) || !aligned16(stats) ||
+      !aligned16(grad) || !aligned16(ws))
+    return BPC_ERR_ALIGNMENT;
+  if (!ws || ws_bytes < distill_workspace(d, rows)) return BPC_ERR_WORKSPACE;
+  DistillCall c = distill_call(d, logits, dtype, row_stride, rows);
+  c.messages = (const uint8_t *)messages;
+  c.labels = labels;
+  c.weight = row_weight;
+  c.loss = loss;
+  c.stats = stats;
+  c.grad = grad;
+  c.grad_stride = grad_stride;
+  return hip_status(distill_run(c, role, (uint8_t *)ws, (hipStream_t)hip_stream));
+}
+
+bpc_status_t bpc_distill_loss(const bpc_distill_t *d, const void *logits, bpc_dtype_t dtype, uint64_t row_stride, uint64_t rows,
+                              const void *messages, const int64_t *labels, const float *row_weight, float *loss, void *stats,
+                              void *ws, size_t ws_bytes, void *hip_stream) {
+  return distill_forward(DistillRole::loss, d, logits, dtype, row_stride, rows, messages, labels, row_weight, loss, stats, nullptr,
+                         0, ws, ws_bytes, hip_stream);
+}
+
+bpc_status_t bpc_distill_step(const bpc_distill_t *d, const void *logits, bpc_dtype_t dtype, uint64_t row_stride, uint64_t rows,
+                              const void *messages, const int64_t *labels, const float *row_weight, float *loss, void *grad,
+                              uint64_t grad_stride, void *ws, size_t ws_bytes, void *hip_stream) {
+  return distill_forward(DistillRole::step, d, logits, dtype, row_stride, rows, messages, labels, row_weight, loss, nullptr, grad,
+                         grad_stride, ws, ws_bytes, hip_stream);
+}
+
+bpc_status_t bpc_distill_grad(const bpc_distill_t *d, const void *logits, bpc_dtype_t dtype, uint64_t row_stride, uint64_t rows,
+                              const void *messages, const int64_t *labels, const float *row_weight, const void *stats, void *grad,
+                              uint64_t grad_stride, void *hip_stream) {
+  const bpc_status_t st = check_rows(d, logits, dtype, row_stride, rows);
+  if (st != BPC_OK) return st;
+  if (grad_stride < d->vocab) return BPC_ERR_INVALID_ARG;
+  if (grad_stride > kMaxRowStride) return BPC_ERR_UNSUPPORTED;
+  if (rows == 0) return BPC_OK;
+  if (!messages || !stats || !grad) return BPC_ERR_INVALID_ARG;
+  if (!aligned16(messages) || !aligned16(labels) || !aligned16(row_weight) || !aligned16(stats) || !aligned16(grad))
+    return BPC_ERR_ALIGNMENT;
+  DistillCall c = distill_call(d, logits, dtype, row_stride, rows);
+  c.messages = (const uint8_t *)messages;
+  c.labels = labels;
+  c.weight = row_weight;
+  c.stats = const_cast<void *>(stats);
+  c.grad = grad;
+  c.grad_stride = grad_stride;
+  return hip_status(distill_run(c, DistillRole::grad, nullptr, (hipStream_t)hip_stream));
 }
 
 bpc_status_t bpc_stream_probe(bpc_probe_t mix, const void *a, const void *b, void *c, uint64_t n, void *hip_stream) {

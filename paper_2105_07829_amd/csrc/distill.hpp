@@ -1,0 +1,165 @@
+// Rows of logits: how a row is cut into 16-byte vectors and chunks, number types, workgroup
+// reductions.  Shared by the teacher's top-k messages (logits_topk.hip) and the student's loss and
+// gradient (distill.hip).
+#pragma once
+#include "device_utils.hpp"
+#include "distill_geometry.hpp"
+
+namespace bpc {
+
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kNegInf = -__builtin_huge_valf();
+
+// One type of logits: E of them fill a 16-byte vector.
+template <int DT> struct Num;
+template <> struct Num<BPC_F32> {
+  using raw = float;
+  static constexpr int E = 4;
+  static __device__ void widen(u32x4 v, float *x) {
+    x[0] = __uint_as_float(v.x); x[1] = __uint_as_float(v.y); x[2] = __uint_as_float(v.z); x[3] = __uint_as_float(v.w);
+  }
+  static __device__ u32x4 narrow(const float *x) { return as_u32x4(x[0], x[1], x[2], x[3]); }
+  static __device__ float get(const raw *p) { return *p; }
+  static __device__ void put(raw *p, float x) { *p = x; }
+};
+template <> struct Num<BPC_F16> {
+  using raw = _Float16;
+  typedef _Float16 x2 __attribute__((ext_vector_type(2)));
+  static constexpr int E = 8;
+  static __device__ void widen(u32x4 v, float *x) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t w = v[i];   // (a vector's component has no address)
+      const x2 h = __builtin_bit_cast(x2, w);
+      x[2 * i] = (float)h.x;
+      x[2 * i + 1] = (float)h.y;
+    }
+  }
+  static __device__ u32x4 narrow(const float *x) {
+    u32x4 v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x2 h;
+      h.x = (_Float16)x[2 * i];
+      h.y = (_Float16)x[2 * i + 1];
+      v[i] = __builtin_bit_cast(uint32_t, h);
+    }
+    return v;
+  }
+  static __device__ float get(const raw *p) { return (float)*p; }
+  static __device__ void put(raw *p, float x) { *p = (_Float16)x; }
+};
+template <> struct Num<BPC_BF16> {
+  using raw = __bf16;
+  typedef __bf16 x2 __attribute__((ext_vector_type(2)));
+  static constexpr int E = 8;
+  static __device__ void widen(u32x4 v, float *x) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = __uint_as_float(v[i] << 16);
+      x[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
+    }
+  }
+  static __device__ u32x4 narrow(const float *x) {   // (rounds to nearest even)
+    u32x4 v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x2 h;
+      h.x = (__bf16)x[2 * i];
+      h.y = (__bf16)x[2 * i + 1];
+      v[i] = __builtin_bit_cast(uint32_t, h);
+    }
+    return v;
+  }
+  static __device__ float get(const raw *p) { return (float)*p; }
+  static __device__ void put(raw *p, float x) { *p = (__bf16)x; }
+};
+
+// 2^x with the hardware's instruction (1 ulp; results below 2^-126 become 0, 2^-inf = 0).
+__device__ inline float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
+// What exponents are taken relative to: m, or 0 where everything is masked (-inf - -inf is no number).
+__device__ inline float ref_of(float m) { return m == kNegInf ? 0.0f : m; }
+
+// A row whose elements start `off` elements into its first 16-byte block: vector v holds elements
+// v * E - off and on.  The first and the last vector may be partial, the others are read whole.
+template <int DT>
+struct Row {
+  using N = Num<DT>;
+  static constexpr int E = N::E;
+  const typename N::raw *p;
+  uint32_t vocab, off, nv;
+  __device__ Row(const void *base, uint64_t row, uint64_t stride, uint32_t vocab_)
+      : p(reinterpret_cast<const typename N::raw *>(base) + uniform_off(row * stride)), vocab(vocab_) {
+    off = (uint32_t)(reinterpret_cast<uintptr_t>(p) & 15) / sizeof(typename N::raw);
+    nv = (off + vocab + E - 1) / E;
+  }
+  __device__ bool whole(uint32_t v) const { return v * E >= off && v * E - off + E <= vocab; }
+  __device__ u32x4 load(uint32_t v) const {   // of a whole vector
+    return __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p + ((int)(v * E) - (int)off)));
+  }
+  // Any vector; what lies outside the row reads as -inf and is not touched.
+  __device__ void load_any(uint32_t v, float *x) const {
+    if (whole(v)) {
+      N::widen(load(v), x);
+    } else {
+#pragma unroll
+      for (int i = 0; i < E; ++i) {
+        const int j = (int)(v * E) - (int)off + i;
+        x[i] = j >= 0 && j < (int)vocab ? N::get(p + j) : kNegInf;
+      }
+    }
+  }
+  // The whole vectors of [v0, v1): [*b0, *b1); a partial first vector is v0 itself, a partial last one v1 - 1.
+  __device__ void body(uint32_t v0, uint32_t v1, uint32_t *b0, uint32_t *b1) const {
+    *b0 = v0 < v1 && !whole(v0) ? v0 + 1 : v0;
+    *b1 = *b0 < v1 && !whole(v1 - 1) ? v1 - 1 : v1;
+  }
+};
+
+// Sum and maximum over a workgroup in a fixed order, in every thread.  `lds`: one float a wave.
+template <int THREADS>
+__device__ inline float all_sum(float x, float *lds) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
+  if (THREADS == 64) return x;
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
+  __syncthreads();
+  float t = 0.0f;
+#pragma unroll
+  for (int w = 0; w < THREADS / 64; ++w) t += lds[w];
+  return t;
+}
+template <int THREADS>
+__device__ inline float all_max(float x, float *lds) {
+  x = wave_max(x);
+  if (THREADS == 64) return x;
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
+  __syncthreads();
+  float t = lds[0];
+#pragma unroll
+  for (int w = 1; w < THREADS / 64; ++w) t = fmaxf(t, lds[w]);
+  return t;
+}
+
+// The fields of a row's record (the record of TOPK / TOPK16 with the mass of the rest and the row's
+// largest logit in the header).
+struct Record {
+  const uint8_t *p;
+  uint32_t val_off;
+  bool half;
+  __device__ Record(const uint8_t *messages, uint64_t row, uint64_t stride, uint32_t k, bool half_)
+      : p(messages + uniform_off(row * stride)), val_off(kHeaderBytes + 4 * (uint32_t)ru4(k)), half(half_) {}
+  __device__ uint32_t count(uint32_t k) const {   // (never more than there is room for, whatever it says)
+    const uint32_t n = *reinterpret_cast<const uint32_t *>(p);
+    return n < k ? n : k;
+  }
+  __device__ float rest() const { return reinterpret_cast<const float *>(p)[1]; }
+  __device__ uint32_t idx(uint32_t e) const { return reinterpret_cast<const uint32_t *>(p + kHeaderBytes)[e]; }
+  __device__ float val(uint32_t e) const {
+    return half ? (float)reinterpret_cast<const _Float16 *>(p + val_off)[e] : reinterpret_cast<const float *>(p + val_off)[e];
+  }
+};
+
+}  // namespace bpc
