@@ -364,7 +364,7 @@ constexpr int kRowThreads = 256;
 template <int DT, int HARD>
 static hipError_t run_typed(Args g, DistillRole role, uint8_t *ws, hipStream_t stream) {
   const uint32_t rows = (uint32_t)g.a.rows;
-  const Cut cut = cut_rows(g.a.rows, g.a.vocab, DT);
+  const Cut cut = cut_rows(g.a.rows, g.a.vocab, DT, g.a.row_stride);
   g.chunks = cut.chunks;
   g.vecs = cut.vecs;
   const DistillWs lay = distill_ws(g.a.rows, cut);

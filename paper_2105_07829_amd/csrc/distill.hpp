@@ -19,6 +19,7 @@ template <> struct Num<BPC_F32> {
     x[0] = __uint_as_float(v.x); x[1] = __uint_as_float(v.y); x[2] = __uint_as_float(v.z); x[3] = __uint_as_float(v.w);
   }
   static __device__ u32x4 narrow(const float *x) { return as_u32x4(x[0], x[1], x[2], x[3]); }
+  static __device__ u32x4 masked() { return u32x4{0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u}; }   // -inf
   static __device__ float get(const raw *p) { return *p; }
   static __device__ void put(raw *p, float x) { *p = x; }
 };
@@ -46,6 +47,7 @@ template <> struct Num<BPC_F16> {
     }
     return v;
   }
+  static __device__ u32x4 masked() { return u32x4{0xfc00fc00u, 0xfc00fc00u, 0xfc00fc00u, 0xfc00fc00u}; }   // -inf
   static __device__ float get(const raw *p) { return (float)*p; }
   static __device__ void put(raw *p, float x) { *p = (_Float16)x; }
 };
@@ -71,6 +73,7 @@ template <> struct Num<BPC_BF16> {
     }
     return v;
   }
+  static __device__ u32x4 masked() { return u32x4{0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u}; }   // -inf
   static __device__ float get(const raw *p) { return (float)*p; }
   static __device__ void put(raw *p, float x) { *p = (__bf16)x; }
 };
@@ -96,6 +99,9 @@ struct Row {
   __device__ bool whole(uint32_t v) const { return v * E >= off && v * E - off + E <= vocab; }
   __device__ u32x4 load(uint32_t v) const {   // of a whole vector
     return __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p + ((int)(v * E) - (int)off)));
+  }
+  __device__ u32x4 load_cached(uint32_t v) const {   // of a whole vector that is read again
+    return *reinterpret_cast<const u32x4 *>(p + ((int)(v * E) - (int)off));
   }
   // Any vector; what lies outside the row reads as -inf and is not touched.
   __device__ void load_any(uint32_t v, float *x) const {

@@ -29,10 +29,11 @@ inline bool distill_built(const bpc_distill_t *d, uint64_t rows) {
 }
 
 inline uint32_t elem_bytes(int dtype) { return dtype == BPC_F32 ? 4 : 2; }
-// Vectors of a row wherever it starts (one more than its elements fill).
-inline uint32_t row_vecs(uint32_t vocab, int dtype) {
+// Vectors of the row that spans most of them: rows may start anywhere in a 16-byte block unless their stride is a
+// multiple of one.
+inline uint32_t row_vecs(uint32_t vocab, int dtype, uint64_t row_stride) {
   const uint32_t e = 16 / elem_bytes(dtype);
-  return (vocab + e - 1) / e + 1;
+  return (uint32_t)cdiv(vocab + (row_stride % e ? e - 1 : 0), e);
 }
 
 // Rows are cut into chunks, a workgroup each, where one workgroup may not have them whole.
@@ -40,9 +41,9 @@ struct Cut {
   uint32_t chunks;   // a row
   uint32_t vecs;     // of a chunk
 };
-inline Cut cut_rows(uint64_t rows, uint32_t vocab, int dtype) {
+inline Cut cut_rows(uint64_t rows, uint32_t vocab, int dtype, uint64_t row_stride) {
   (void)rows;
-  const uint32_t nv = row_vecs(vocab, dtype);
+  const uint32_t nv = row_vecs(vocab, dtype, row_stride);
   Cut c;
   c.chunks = (uint32_t)cdiv(nv, kChunkVecs);
   c.vecs = (uint32_t)cdiv(nv, c.chunks);
@@ -72,8 +73,10 @@ inline DistillWs distill_ws(uint64_t rows, const Cut &cut) {
 inline size_t distill_workspace(const bpc_distill_t *d, uint64_t rows) {
   size_t most = 256;
   for (int dtype = BPC_F32; dtype <= BPC_BF16; ++dtype) {
-    const size_t s = distill_ws(rows, cut_rows(rows, d->vocab, dtype)).total;
-    if (s > most) most = s;
+    for (uint64_t stride = 0; stride < 2; ++stride) {   // aligned rows and others
+      const size_t s = distill_ws(rows, cut_rows(rows, d->vocab, dtype, stride)).total;
+      if (s > most) most = s;
+    }
   }
   return most;
 }

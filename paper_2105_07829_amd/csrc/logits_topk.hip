@@ -23,6 +23,8 @@ __device__ inline uint32_t order_key(float x) {
   return x != x ? 0xffffffffu : x == kNegInf ? 0u : k;
 }
 
+constexpr uint32_t kLowestKey = 0x00800000u;   // of the lowest finite number
+
 // Writes the entries of a record from n on (idx -1, val -inf) and its header.
 template <int THREADS>
 __device__ void close_record(const TeacherArgs &g, uint8_t *rec, uint32_t n, float rest, float top) {
@@ -132,22 +134,465 @@ __device__ void select_any(const TeacherArgs &g, const Row<DT> &row, uint8_t *re
   close_record<THREADS>(g, rec, listed, rest, top);
 }
 
-template <int DT, int THREADS>
-__global__ __launch_bounds__(THREADS) void logits_topk_kernel(TeacherArgs g) {
+// ---- rows whose k-th largest logit can be bounded from below by largest logits of groups
+
+__device__ inline float key_value(uint32_t key) {   // of a key that is neither 0 nor a NaN's
+  return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key);
+}
+
+// How many of a wave's keys reach `least`: a comparison each, the counting is the scalar unit's.
+__device__ inline uint32_t wave_count(uint32_t key, uint32_t least) { return (uint32_t)__popcll(__ballot(key >= least)); }
+
+// The k-th largest of n keys (1 <= k): the largest key that at least k of them reach, or 0 if fewer than k
+// reach `lo`.  No key is above `hi`.  Stops as soon as a key is found that no more than k + slack reach (slack 0:
+// the keys that reach it are those that reach the k-th largest all the same).  *reach: how many reach the answer.
+// count(least): how many keys reach `least`, the same in every thread.
+template <class Count>
+__device__ uint32_t kth_key(const Count &count, uint32_t k, uint32_t lo, uint32_t hi, uint32_t slack, uint32_t *reach) {
+  uint32_t at = count(lo);
+  if (at < k) {
+    *reach = at;
+    return 0;
+  }
+  while (lo < hi && at > k + slack) {
+    const uint32_t mid = lo + (hi - lo) / 2 + ((hi - lo) & 1);
+    const uint32_t c = count(mid);
+    if (c >= k) {
+      lo = mid;
+      at = c;
+    } else {
+      hi = mid - 1;
+    }
+  }
+  *reach = at;
+  return lo;
+}
+
+// Adds up the waves' counts with one barrier a count: three counters take turns, each is cleared behind the barrier
+// after the one that it was read behind.  (All threads, a barrier before the first add and before the next Tally.)
+struct Tally {
+  uint32_t *counters, turn = 0;
+  __device__ explicit Tally(uint32_t *lds) : counters(lds) {
+    if (threadIdx.x < 3) counters[threadIdx.x] = 0;
+    __syncthreads();
+  }
+  __device__ uint32_t add(uint32_t wave_total) {
+    if ((threadIdx.x & 63) == 0 && wave_total) atomicAdd(&counters[turn], wave_total);
+    __syncthreads();
+    const uint32_t all = counters[turn];
+    turn = turn == 2 ? 0 : turn + 1;
+    if (threadIdx.x == 0) counters[turn == 2 ? 0 : turn + 1] = 0;
+    return all;
+  }
+};
+
+constexpr int kTopThreads = 256;
+
+// What exponents of base 2 are taken relative to: the largest logit times c2, as f32 rounds it.  Any reference will
+// do as long as all parties to a sum know it, so the rounding costs nothing, and x * c2 - reference is one
+// instruction, with one rounding.  Below -2^20 (masked by -inf or by a type's lowest value) it stays there: 2^x is 0
+// next to any row that is handled so.
+constexpr float kLowRef = -0x1p20f;
+__device__ inline float base2_ref(float m, float c2) { return fmaxf(m * c2, kLowRef); }
+__device__ inline float base2_exp(float x, float c2, float ref2) { return exp2_hw(__builtin_fmaf(x, c2, -ref2)); }
+// Rows whose largest logit is further from 0 than this (or NaN, or infinite) go the other way: the rounding of the
+// reference would be felt.
+constexpr float kFarRef = 0x1p16f;
+
+// Rows by groups.  One pass finds every group's largest logit and its sum of exponentials (relative to that logit); at
+// least k logits reach the k-th largest of the groups' largest (or a little less), so only the few groups that reach
+// it are looked through again for candidates.  A thread loads four vectors at a time, kTopThreads apart; PER of them
+// (1, 2, or 4 in each of 1 << shift such loads) make a group.
+template <int DT, int PER>
+__global__ __launch_bounds__(kTopThreads) void logits_topk_groups_kernel(TeacherArgs g, uint32_t shift, uint32_t n_groups, uint32_t cap) {
+  constexpr int E = Num<DT>::E, T = kTopThreads, Q = 4 / PER;
+  extern __shared__ __align__(16) uint8_t dyn[];
+  __shared__ float lds[T / 64], lds_min[T / 64];
+  __shared__ uint32_t counters[3], scan_lds[T / 64], before[T];
+  __shared__ uint32_t n_cand, pick[2];
+  __shared__ unsigned long long left_sum;
   const uint64_t r = blockIdx.x;
   uint8_t *rec = g.out + uniform_off(r * g.a.message_stride);
   if (g.a.weight && uniform_load(g.a.weight + r) == 0.0f) {
-    close_record<THREADS>(g, rec, 0, 0.0f, kNegInf);
+    close_record<T>(g, rec, 0, 0.0f, kNegInf);
     return;
   }
   const Row<DT> row(g.a.logits, r, g.a.row_stride, g.a.vocab);
-  select_any<DT, THREADS>(g, row, rec);
+  uint32_t *gkey = reinterpret_cast<uint32_t *>(dyn);
+  float *gsum = reinterpret_cast<float *>(gkey + n_groups);
+  uint32_t *ckey = reinterpret_cast<uint32_t *>(gsum + n_groups);
+  uint32_t *cidx = ckey + cap;
+  uint16_t *glist = reinterpret_cast<uint16_t *>(cidx + cap);
+  uint32_t b0, b1;
+  row.body(0, row.nv, &b0, &b1);
+  const uint32_t loads = (b1 - b0 + 4 * T - 1) / (4 * T), whole_loads = (b1 - b0) / (4 * T);
+  const float c2 = g.c2;
+  float top = kNegInf;
+  uint32_t done = 0;   // groups written
+  float m = kNegInf, s = 0.0f;
+  for (uint32_t b = 0; b < loads; ++b) {
+    u32x4 w[4];
+    const uint32_t v0 = b0 + b * 4 * T + threadIdx.x;
+    if (b < whole_loads) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) w[u] = row.load_cached(v0 + u * T);
+    } else {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) w[u] = v0 + u * T < b1 ? row.load_cached(v0 + u * T) : Num<DT>::masked();
+    }
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      float x[PER * E];
+#pragma unroll
+      for (int u = 0; u < PER; ++u) Num<DT>::widen(w[q * PER + u], x + u * E);
+      float nm = PER == 4 ? m : kNegInf;
+#pragma unroll
+      for (int i = 0; i < PER * E; ++i) nm = fmaxf(nm, x[i]);
+      const float ref2 = base2_ref(nm, c2);
+      float ns = PER == 4 ? s * exp2_hw(base2_ref(m, c2) - ref2) : 0.0f;
+#pragma unroll
+      for (int i = 0; i < PER * E; ++i) ns += base2_exp(x[i], c2, ref2);
+      m = nm;
+      s = ns;
+      if (PER != 4 || ((b + 1) & ((1u << shift) - 1)) == 0 || b + 1 == loads) {
+        gkey[done + threadIdx.x] = order_key(m);
+        gsum[done + threadIdx.x] = s;
+        top = fmaxf(top, m);
+        done += T;
+        m = kNegInf;
+        s = 0.0f;
+      }
+    }
+  }
+  for (; done < n_groups; done += T) {
+    gkey[done + threadIdx.x] = 0;
+    gsum[done + threadIdx.x] = 0.0f;
+  }
+  // every thread's largest logit is the largest of some groups: T of them reach the smallest of those
+  float least = -wave_max(-top);
+  // the partial vectors at the ends are nobody's group: they are looked through in any case
+  float edge[E];
+  const bool has_edge = (threadIdx.x == 0 && b0 > 0) || (threadIdx.x == 1 && b1 < row.nv);
+  const uint32_t edge_v = threadIdx.x == 0 ? 0 : row.nv - 1;
+  bool odd = false;
+  if (has_edge) {
+    row.load_any(edge_v, edge);
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      top = fmaxf(top, edge[i]);
+      odd = odd || edge[i] != edge[i];
+    }
+  }
+  if ((threadIdx.x & 63) == 0) lds_min[threadIdx.x >> 6] = least;
+  if (threadIdx.x == 0) {
+    n_cand = 0;
+    left_sum = 0;
+  }
+  top = all_max<T>(top, lds);
+  least = lds_min[0];
+#pragma unroll
+  for (int i = 1; i < T / 64; ++i) least = fminf(least, lds_min[i]);
+  const float top2 = base2_ref(top, c2);
+  uint32_t low = 0, reach;
+  {
+    // a lower bound of the k-th largest logit: k groups reach it
+    Tally tally(counters);
+    const uint4 *quad = reinterpret_cast<const uint4 *>(gkey);
+    const auto count = [&](uint32_t key) {
+      uint32_t c = 0;
+      for (uint32_t i = threadIdx.x; i < n_groups / 4; i += T) {
+        const uint4 q = quad[i];
+        c += wave_count(q.x, key) + wave_count(q.y, key) + wave_count(q.z, key) + wave_count(q.w, key);
+      }
+      return tally.add(c);
+    };
+    const uint32_t from = g.a.k <= T && least > kNegInf ? order_key(least) : kLowestKey;
+    low = kth_key(count, g.a.k, from, order_key(top), g.a.k / 8 + 4, &reach);
+    if (low == 0) low = kLowestKey;
+  }
+  float rest = 0.0f;   // relative to 2^top2
+  uint32_t mine = 0, n_listed;
+  for (uint32_t i = threadIdx.x; i < n_groups; i += T) {
+    const uint32_t key = gkey[i];
+    const float sum = gsum[i];
+    odd = odd || sum != sum;
+    if (key >= low) ++mine;
+    else if (key != 0) rest += sum * exp2_hw(base2_ref(key_value(key), c2) - top2);
+  }
+  // (listed by a prefix sum, so that the sum over what these groups hold beside the candidates is always formed in
+  // the same order)
+  uint32_t at = block_exclusive_scan<T>(mine, scan_lds, &n_listed);
+  for (uint32_t i = threadIdx.x; mine && i < n_groups; i += T)
+    if (gkey[i] >= low) glist[at++] = (uint16_t)i;
+  if (__syncthreads_or(odd || !(fabsf(top * c2) < kFarRef))) {   // a NaN, an infinity, numbers far from 0, nothing at all
+    select_any<DT, T>(g, row, rec);
+    return;
+  }
+  const float low_value = key_value(low);
+  const auto look = [&](const float *x, uint32_t j0) {
+    float most = x[0];
+#pragma unroll
+    for (int i = 1; i < E; ++i) most = fmaxf(most, x[i]);
+#pragma unroll
+    for (int i = 0; i < E; ++i) rest += x[i] >= low_value ? 0.0f : base2_exp(x[i], c2, top2);
+    if (most >= low_value) {
+#pragma unroll
+      for (int i = 0; i < E; ++i) {
+        if (x[i] >= low_value) {
+          const uint32_t to = atomicAdd(&n_cand, 1u);
+          if (to < cap) {
+            ckey[to] = order_key(x[i]);
+            cidx[to] = j0 + i;
+          }
+        }
+      }
+    }
+  };
+  const uint32_t vg_shift = (PER == 1 ? 0 : PER == 2 ? 1 : 2) + shift;
+  const uint32_t pairs = n_listed << vg_shift;
+  for (uint32_t p = threadIdx.x; p < pairs; p += T) {
+    const uint32_t id = glist[p >> vg_shift], u = p & ((1u << vg_shift) - 1);
+    const uint32_t v = b0 + (((id / T) << vg_shift) + u) * T + id % T;
+    if (v < b1) {
+      float x[E];
+      Num<DT>::widen(row.load_cached(v), x);
+      look(x, v * E - row.off);
+    }
+  }
+  if (has_edge) look(edge, edge_v * E - row.off);
+  __syncthreads();
+  const uint32_t cand = n_cand;
+  if (cand > cap) {   // more logits level with the bound than there is room for
+    __syncthreads();
+    select_any<DT, T>(g, row, rec);
+    return;
+  }
+  const uint32_t take = cand < g.a.k ? cand : g.a.k;
+  // candidates to list: those above `kth`, and of those level with it the ones up to index `last`
+  uint32_t kth = low, last = 0xffffffffu;
+  if (take < cand) {
+    constexpr uint32_t kOneWave = 512;
+    const uint32_t high = order_key(top);
+    const auto search = [&](const auto &count_keys, const auto &count_level) {
+      kth = kth_key(count_keys, take, low, high, 0, &reach);
+      if (reach > take) {
+        // too many are level with the k-th: out go those with the highest indices
+        const uint32_t above = kth == 0xffffffffu ? 0u : count_keys(kth + 1);
+        last = ~kth_key(count_level, take - above, 1u, 0xffffffffu, 0, &reach);
+      }
+    };
+    if (cand <= kOneWave) {   // (uniform) by one wave, out of its registers
+      if (threadIdx.x < 64) {
+        uint32_t key[kOneWave / 64];
+#pragma unroll
+        for (uint32_t i = 0; i < kOneWave / 64; ++i) {
+          const uint32_t e = threadIdx.x + i * 64;
+          key[i] = e < cand ? ckey[e] : 0u;
+        }
+        const auto count_keys = [&](uint32_t least_key) {
+          uint32_t c = 0;
+#pragma unroll
+          for (uint32_t i = 0; i < kOneWave / 64; ++i) c += wave_count(key[i], least_key);
+          return c;
+        };
+        const auto count_level = [&](uint32_t least_key) {
+          uint32_t c = 0;
+          for (uint32_t i = 0; i < kOneWave / 64; ++i) {
+            const uint32_t e = threadIdx.x + i * 64;
+            c += wave_count(e < cand && ckey[e] == kth ? ~cidx[e] : 0u, least_key);
+          }
+          return c;
+        };
+        search(count_keys, count_level);
+        if (threadIdx.x == 0) {
+          pick[0] = kth;
+          pick[1] = last;
+        }
+      }
+      __syncthreads();
+      kth = pick[0];
+      last = pick[1];
+    } else {
+      Tally tally(counters);
+      const uint32_t rounds = (cand + T - 1) / T;
+      const auto count_keys = [&](uint32_t least_key) {
+        uint32_t c = 0;
+        for (uint32_t i = 0; i < rounds; ++i) {
+          const uint32_t e = threadIdx.x + i * T;
+          c += wave_count(e < cand ? ckey[e] : 0u, least_key);
+        }
+        return tally.add(c);
+      };
+      const auto count_level = [&](uint32_t least_key) {
+        uint32_t c = 0;
+        for (uint32_t i = 0; i < rounds; ++i) {
+          const uint32_t e = threadIdx.x + i * T;
+          c += wave_count(e < cand && ckey[e] == kth ? ~cidx[e] : 0u, least_key);
+        }
+        return tally.add(c);
+      };
+      search(count_keys, count_level);
+    }
+  }
+  // index order: a bit a logit for what is listed (in place of the groups), a prefix sum over stretches of words
+  uint32_t *bits = gkey;
+  const uint32_t span = (row.nv * E + 32 * T - 1) / (32 * T);   // words of a thread's stretch
+  for (uint32_t i = threadIdx.x; i < span * T; i += T) bits[i] = 0;
+  __syncthreads();
+  const auto listed = [&](uint32_t i) { return ckey[i] > kth || (ckey[i] == kth && cidx[i] <= last); };
+  float over = kNegInf;   // the largest candidate that is not listed
+  for (uint32_t i = threadIdx.x; i < cand; i += T) {
+    if (listed(i)) atomicOr(&bits[cidx[i] >> 5], 1u << (cidx[i] & 31));
+    else over = fmaxf(over, key_value(ckey[i]));
+  }
+  __syncthreads();
+  {
+    uint32_t n = 0, all;
+    for (uint32_t i = 0; i < span; ++i) n += __popc(bits[threadIdx.x * span + i]);
+    before[threadIdx.x] = block_exclusive_scan<T>(n, scan_lds, &all);
+  }
+  if (take < cand) {
+    // the candidates lie in any order: the sum of those not listed is formed in whole numbers, 2^-40 of the largest
+    over = base2_ref(all_max<T>(over, lds), c2);
+    unsigned long long sum = 0;
+    for (uint32_t i = threadIdx.x; i < cand; i += T)
+      if (!listed(i)) sum += (unsigned long long)(base2_exp(key_value(ckey[i]), c2, over) * 0x1p40f);
+    if (sum) atomicAdd(&left_sum, sum);
+  }
+  __syncthreads();
+  for (uint32_t i = threadIdx.x; i < cand; i += T) {
+    if (!listed(i)) continue;
+    const uint32_t j = cidx[i], word = j >> 5, stretch = word / span;
+    uint32_t place = before[stretch];
+    for (uint32_t q = stretch * span; q < word; ++q) place += __popc(bits[q]);
+    place += __popc(bits[word] & ((1u << (j & 31)) - 1));
+    if (place < g.a.k) put_entry(g, rec, place, j, key_value(ckey[i]) - top);
+  }
+  rest = all_sum<T>(rest, lds);
+  if (take < cand) rest += (float)left_sum * 0x1p-40f * exp2_hw(over - top2);
+  // (from the rounded reference to the largest logit itself)
+  close_record<T>(g, rec, take, rest * exp2_hw(-__builtin_fmaf(top, c2, -top2)), top);
+}
+
+// ---- short rows of which many logits are listed: the whole row in LDS
+
+constexpr uint32_t kDenseVocab = 15360;   // (60 KB)
+
+template <int DT>
+__global__ __launch_bounds__(kTopThreads) void logits_topk_dense_kernel(TeacherArgs g) {
+  constexpr int E = Num<DT>::E, T = kTopThreads;
+  extern __shared__ __align__(16) uint8_t dyn[];
+  __shared__ float lds[T / 64];
+  __shared__ uint32_t counters[3], scan_lds[T / 64];
+  const uint64_t r = blockIdx.x;
+  uint8_t *rec = g.out + uniform_off(r * g.a.message_stride);
+  if (g.a.weight && uniform_load(g.a.weight + r) == 0.0f) {
+    close_record<T>(g, rec, 0, 0.0f, kNegInf);
+    return;
+  }
+  const Row<DT> row(g.a.logits, r, g.a.row_stride, g.a.vocab);
+  float *x = reinterpret_cast<float *>(dyn);
+  const uint32_t n = g.a.vocab;
+  float top = kNegInf;
+  bool nan = false;
+  for (uint32_t v = threadIdx.x; v < row.nv; v += T) {
+    float y[E];
+    row.load_any(v, y);
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      const uint32_t j = v * E - row.off + i;
+      if (j < n) x[j] = y[i];
+      top = fmaxf(top, y[i]);
+      nan = nan || y[i] != y[i];
+    }
+  }
+  top = all_max<T>(top, lds);
+  if (__syncthreads_or(nan)) top = __builtin_nanf("");
+  const float ref = ref_of(top);
+  uint32_t reach;
+  Tally tally(counters);
+  const uint32_t rounds = (n + T - 1) / T;
+  const auto count = [&](uint32_t key) {
+    uint32_t c = 0;
+    for (uint32_t i = 0; i < rounds; ++i) {
+      const uint32_t j = threadIdx.x + i * T;
+      c += wave_count(j < n ? order_key(x[j]) : 0u, key);
+    }
+    return tally.add(c);
+  };
+  const uint32_t kth = kth_key(count, g.a.k, kLowestKey, order_key(top), 0, &reach);
+  // each thread a stretch of the row, of odd length (so that the threads of a wave are in different banks)
+  const uint32_t len = ((n + T - 1) / T) | 1u;
+  const uint32_t lo = threadIdx.x * len < n ? threadIdx.x * len : n, hi = lo + len < n ? lo + len : n;
+  uint32_t above = 0, same = 0;
+  for (uint32_t j = lo; j < hi; ++j) {
+    const uint32_t key = order_key(x[j]);
+    above += key > kth ? 1u : 0u;
+    same += key == kth && key != 0 ? 1u : 0u;
+  }
+  uint32_t all_above, all;
+  uint32_t at = block_exclusive_scan<T>(above, scan_lds, &all_above);
+  const uint32_t same_before = block_exclusive_scan<T>(same, scan_lds, &all);
+  // of the logits level with the k-th the first `open` are listed
+  const uint32_t open = all_above < g.a.k ? g.a.k - all_above : 0;
+  at += same_before < open ? same_before : open;
+  uint32_t left = same_before < open ? open - same_before : 0;
+  float rest = 0.0f;
+  for (uint32_t j = lo; j < hi; ++j) {
+    const uint32_t key = order_key(x[j]);
+    bool take = key > kth;
+    if (key == kth && key != 0 && left > 0) {
+      take = true;
+      --left;
+    }
+    if (take) put_entry(g, rec, at++, j, x[j] - ref);
+    else if (key != 0) rest += exp2_hw((x[j] - ref) * g.c2);
+  }
+  rest = all_sum<T>(rest, lds);
+  close_record<T>(g, rec, all_above + (all < open ? all : open), rest, top);
+}
+
+// Rows of any length by the radix select alone.
+template <int DT>
+__global__ __launch_bounds__(kTopThreads) void logits_topk_any_kernel(TeacherArgs g) {
+  const uint64_t r = blockIdx.x;
+  uint8_t *rec = g.out + uniform_off(r * g.a.message_stride);
+  if (g.a.weight && uniform_load(g.a.weight + r) == 0.0f) {
+    close_record<kTopThreads>(g, rec, 0, 0.0f, kNegInf);
+    return;
+  }
+  const Row<DT> row(g.a.logits, r, g.a.row_stride, g.a.vocab);
+  select_any<DT, kTopThreads>(g, row, rec);
+}
+
+template <int DT, int PER>
+static hipError_t run_groups(const TeacherArgs &g, uint32_t shift, uint32_t n_groups, hipStream_t stream) {
+  const uint32_t cap = g.a.k <= 512 ? 1024 : 2 * (uint32_t)ru4(g.a.k);
+  // (the bits that later take the place of the groups' keys and sums: at most a word for each vector, a load of four
+  // vectors a thread at most is half a group or more, so 8 bytes a group are enough)
+  const uint32_t dyn = 8 * n_groups + 8 * cap + 2 * n_groups;
+  logits_topk_groups_kernel<DT, PER><<<(uint32_t)g.a.rows, kTopThreads, dyn, stream>>>(g, shift, n_groups, cap);
+  return hipGetLastError();
 }
 
 template <int DT>
 static hipError_t run_typed(const TeacherArgs &g, hipStream_t stream) {
-  logits_topk_kernel<DT, 256><<<(uint32_t)g.a.rows, 256, 0, stream>>>(g);
-  return hipGetLastError();
+  const uint32_t nv = row_vecs(g.a.vocab, DT, g.a.row_stride), T = kTopThreads;
+  if (nv > kChunkVecs) {
+    logits_topk_any_kernel<DT><<<(uint32_t)g.a.rows, kTopThreads, 0, stream>>>(g);
+    return hipGetLastError();
+  }
+  if (nv < 2 * g.a.k && g.a.vocab <= kDenseVocab) {
+    logits_topk_dense_kernel<DT><<<(uint32_t)g.a.rows, kTopThreads, 4 * g.a.vocab, stream>>>(g);
+    return hipGetLastError();
+  }
+  // (whole loads of four vectors, so that the groups of all threads are written)
+  const uint32_t most = g.a.k <= 512 ? 2048 : 4096, loads = (uint32_t)cdiv(nv, 4 * T);
+  if (nv <= most) return run_groups<DT, 1>(g, 0, loads * 4 * T, stream);
+  if (nv <= 2 * most) return run_groups<DT, 2>(g, 0, loads * 2 * T, stream);
+  uint32_t shift = 0;
+  while ((loads >> shift) * T > most) ++shift;
+  return run_groups<DT, 4>(g, shift, (uint32_t)cdiv(loads, 1u << shift) * T, stream);
 }
 
 hipError_t logits_topk(const DistillCall &call, uint8_t *out, uint8_t *ws, hipStream_t stream) {
