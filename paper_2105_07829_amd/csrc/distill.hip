@@ -30,11 +30,67 @@ struct Args {
   uint32_t chunks, vecs;
 };
 
-// Sums of a set of words relative to the largest of them.
+// Largest of a set of logits and the sums of their exponentials relative to it.
 struct Part {
   float m = kNegInf, s = 0.0f, h = 0.0f;
+};
+
+// A bit a word of a stretch of a row: listed.  `bits` starts at vector v0.
+template <int DT>
+struct Marks {
+  static constexpr int E = Num<DT>::E;
+  const uint8_t *bits;   // NULL: nothing is marked
+  uint32_t v0;
+  __device__ bool apply(uint32_t v, float *x) const {   // marked words count as masked; whether there are any
+    if (!bits) return false;
+    const uint32_t i = v - v0;
+    const uint32_t b = E == 8 ? bits[i] : (bits[i >> 1] >> (4 * (i & 1))) & 15u;
+    if (b) {
+#pragma unroll
+      for (int k = 0; k < E; ++k) x[k] = (b >> k) & 1 ? kNegInf : x[k];
+    }
+    return b != 0;
+  }
+};
+
+// ---- sums over a stretch of a row, each thread its own
+
+// With references of base 2 (see base2_ref).  TWO: at temperature 1, too.
+struct FastSum : Part {
+  template <bool TWO, int N>
+  __device__ void add(const float *x, float c2) {
+    float nm = m;
+#pragma unroll
+    for (int i = 0; i < N; ++i) nm = fmaxf(nm, x[i]);
+    const float ref = base2_ref(nm, c2), ref1 = base2_ref(nm, kLog2e);
+    s *= exp2_hw(base2_ref(m, c2) - ref);
+    if (TWO) h *= exp2_hw(base2_ref(m, kLog2e) - ref1);
+    m = nm;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      s += base2_exp(x[i], c2, ref);
+      if (TWO) h += base2_exp(x[i], kLog2e, ref1);
+    }
+  }
+  // relative to the largest of all threads' instead
   template <bool TWO>
-  __device__ void rescale(float nm, float c2) {
+  __device__ void move_to(float all, float c2) {
+    s *= exp2_hw(base2_ref(m, c2) - base2_ref(all, c2));
+    if (TWO) h *= exp2_hw(base2_ref(m, kLog2e) - base2_ref(all, kLog2e));
+    m = all;
+  }
+  // ... and to that logit itself, not its rounded multiple
+  template <bool TWO>
+  __device__ void settle(float c2) {
+    if (m == kNegInf) return;
+    s *= exp2_hw(-__builtin_fmaf(m, c2, -base2_ref(m, c2)));
+    if (TWO) h *= exp2_hw(-__builtin_fmaf(m, kLog2e, -base2_ref(m, kLog2e)));
+  }
+};
+// With differences formed first: for rows whose largest logit is far from 0 (a type's lowest value among them).
+struct PlainSum : Part {
+  template <bool TWO>
+  __device__ void move_to(float nm, float c2) {
     const float d = m - ref_of(nm);
     s *= exp2_hw(d * c2);
     if (TWO) h *= exp2_hw(d * kLog2e);
@@ -45,7 +101,7 @@ struct Part {
     float nm = m;
 #pragma unroll
     for (int i = 0; i < N; ++i) nm = fmaxf(nm, x[i]);
-    rescale<TWO>(nm, c2);
+    move_to<TWO>(nm, c2);
     const float ref = ref_of(nm);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
@@ -56,337 +112,663 @@ struct Part {
   }
 };
 
-template <int DT>
-struct Marks {   // a bit a word of a chunk: listed
-  static constexpr int E = Num<DT>::E;
-  const uint8_t *bits;
-  uint32_t v0;
-  __device__ uint32_t of(uint32_t v) const {
-    const uint32_t i = v - v0;
-    return E == 8 ? bits[i] : (bits[i >> 1] >> (4 * (i & 1))) & 15u;
+// The partial vectors at the ends of the stretch [v0, v1) whose whole vectors are [b0, b1): one thread each.
+template <int DT, bool TWO, class Sum>
+__device__ void add_edges(const Row<DT> &row, uint32_t v0, uint32_t v1, uint32_t b0, uint32_t b1, const Marks<DT> &marks, float c2, Sum *p) {
+  if ((threadIdx.x == 0 && b0 > v0) || (threadIdx.x == 1 && b1 < v1)) {
+    const uint32_t v = threadIdx.x == 0 ? v0 : v1 - 1;
+    float x[Num<DT>::E];
+    row.load_any(v, x);
+    marks.apply(v, x);
+    p->template add<TWO, Num<DT>::E>(x, c2);
   }
-};
+}
 
-// Sums over the vectors [v0, v1) of a row, without the marked words, in every thread.
-template <int DT, bool TWO, int THREADS>
-__device__ Part scan(const Row<DT> &row, uint32_t v0, uint32_t v1, bool marked, const Marks<DT> &marks, float c2, float *lds) {
+// A thread's share of the vectors [v0, v1): four loads at a time.
+template <int DT, bool TWO, int T>
+__device__ FastSum scan(const Row<DT> &row, uint32_t v0, uint32_t v1, const Marks<DT> &marks, float c2) {
   constexpr int E = Num<DT>::E;
-  Part p;
+  FastSum p;
   uint32_t b0, b1;
   row.body(v0, v1, &b0, &b1);
-  const auto one = [&](uint32_t v, float *x) {
-    if (marked) {
-      const uint32_t bits = marks.of(v);
-      if (bits) {
+  uint32_t v = b0 + threadIdx.x;
+  for (uint32_t all = (b1 - b0) / (4 * T); all > 0; --all, v += 4 * T) {
+    u32x4 w[4];
 #pragma unroll
-        for (int i = 0; i < E; ++i) x[i] = (bits >> i) & 1 ? kNegInf : x[i];
-      }
+    for (int u = 0; u < 4; ++u) w[u] = row.load(v + u * T);
+    float x[4 * E];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      Num<DT>::widen(w[u], x + u * E);
+      marks.apply(v + u * T, x + u * E);
     }
-  };
-  for (uint32_t v = b0 + threadIdx.x; v < b1; v += THREADS) {
+    p.add<TWO, 4 * E>(x, c2);
+  }
+  for (; v < b1; v += T) {
     float x[E];
     Num<DT>::widen(row.load(v), x);
-    one(v, x);
+    marks.apply(v, x);
     p.add<TWO, E>(x, c2);
   }
-  const bool first = b0 > v0, last = b1 < v1;
-  if ((threadIdx.x == 0 && first) || (threadIdx.x == 1 && last)) {
-    const uint32_t v = threadIdx.x == 0 ? v0 : v1 - 1;
+  add_edges<DT, TWO>(row, v0, v1, b0, b1, marks, c2, &p);
+  return p;
+}
+template <int DT, bool TWO, int T>
+__device__ PlainSum scan_plain(const Row<DT> &row, uint32_t v0, uint32_t v1, const Marks<DT> &marks, float c2) {
+  constexpr int E = Num<DT>::E;
+  PlainSum p;
+  uint32_t b0, b1;
+  row.body(v0, v1, &b0, &b1);
+  for (uint32_t v = b0 + threadIdx.x; v < b1; v += T) {
     float x[E];
-    row.load_any(v, x);
-    one(v, x);
+    Num<DT>::widen(row.load(v), x);
+    marks.apply(v, x);
     p.add<TWO, E>(x, c2);
   }
-  p.rescale<TWO>(all_max<THREADS>(p.m, lds), c2);
-  p.s = all_sum<THREADS>(p.s, lds);
-  if (TWO) p.h = all_sum<THREADS>(p.h, lds);
+  add_edges<DT, TWO>(row, v0, v1, b0, b1, marks, c2, &p);
   return p;
 }
 
-// Marks the listed words of the vectors [v0, v1).
-template <int DT, int THREADS>
-__device__ void mark(const Args &g, const Row<DT> &row, uint64_t r, uint32_t v0, uint32_t v1, uint32_t *bits) {
-  constexpr int E = Num<DT>::E;
-  const Record rec(g.a.messages, r, g.a.message_stride, g.a.k, g.a.half);
-  const uint32_t n = rec.count(g.a.k), words = ((v1 - v0) * E + 31) / 32;
-  for (uint32_t w = threadIdx.x; w < words; w += THREADS) bits[w] = 0;
-  __syncthreads();
-  for (uint32_t e = threadIdx.x; e < n; e += THREADS) {
-    const uint32_t j = rec.idx(e);
-    const uint32_t at = j + row.off - v0 * E;   // (from the first word of vector v0)
-    if (j < g.a.vocab && j + row.off >= v0 * E && at < (v1 - v0) * E) atomicOr(&bits[at >> 5], 1u << (at & 31));
-  }
-  __syncthreads();
-}
+// ---- exchanges between the waves of a workgroup: sums of N values and maxima of M, in every thread
 
-__device__ inline bool hard_label(const Args &g, uint64_t r, uint32_t *label) {
-  if (!g.a.labels || g.a.hard == 0.0f) return false;
-  const int64_t l = g.a.labels[r];
-  if (l < 0 || l >= (int64_t)g.a.vocab) return false;
-  *label = (uint32_t)l;
-  return true;
-}
-
-// The row's loss and statistics from the sums of its unlisted words (TAIL_DROP: of all words).
-// HARD: 0 no hard term, 1 at the same temperature as the soft one, 2 at its own.
-template <int DT, int HARD, int THREADS>
-__device__ Stats finish(const Args &g, const Row<DT> &row, uint64_t r, Part p, float weight, float *loss, float *lds) {
-  const bool rest_too = g.a.rest_too;
-  const Record rec(g.a.messages, r, g.a.message_stride, g.a.k, g.a.half);
-  const uint32_t n = rec.count(g.a.k);
-  float m = kNegInf, q = 0.0f;
-  for (uint32_t e = threadIdx.x; e < n; e += THREADS) {
-    const uint32_t j = rec.idx(e);
-    if (j >= g.a.vocab) continue;
-    m = fmaxf(m, Num<DT>::get(row.p + j));
-    q += exp2_hw(rec.val(e) * g.c2);
-  }
-  m = all_max<THREADS>(m, lds);
-  q = all_sum<THREADS>(q, lds);
-  Stats st;
-  const float rest = rest_too ? rec.rest() : 0.0f;
-  q += rest;
-  if (n == 0) q = 0.0f;
-  st.m_r = p.m;
-  float z = p.s, h = HARD == 1 ? p.s : p.h;
-  if (rest_too) {
-    st.m = fmaxf(m, p.m);
-    const float ref = ref_of(st.m);
-    float zs = 0.0f, hs = 0.0f;
-    for (uint32_t e = threadIdx.x; e < n; e += THREADS) {
-      const uint32_t j = rec.idx(e);
-      if (j >= g.a.vocab) continue;
-      const float d = Num<DT>::get(row.p + j) - ref;
-      zs += exp2_hw(d * g.c2);
-      if (HARD == 2) hs += exp2_hw(d * kLog2e);
+template <int T, int N, int M>
+struct Exchange {
+  float v[T / 64][N + M];
+  __device__ void all(float *sums, float *most) {   // (one barrier; each Exchange is used once)
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) sums[i] += __shfl_xor(sums[i], o, 64);
+#pragma unroll
+    for (int i = 0; i < M; ++i) most[i] = wave_max(most[i]);
+    if (T == 64) return;
+    if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[threadIdx.x >> 6][i] = sums[i];
+#pragma unroll
+      for (int i = 0; i < M; ++i) v[threadIdx.x >> 6][N + i] = most[i];
     }
-    zs = all_sum<THREADS>(zs, lds);
-    z = p.s * exp2_hw((p.m - ref) * g.c2) + zs;
-    h = z;
-    if (HARD == 2) h = p.h * exp2_hw((p.m - ref) * kLog2e) + all_sum<THREADS>(hs, lds);
-  } else {
-    st.m = p.m;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      float t = 0.0f;
+#pragma unroll
+      for (int w = 0; w < T / 64; ++w) t += v[w][i];
+      sums[i] = t;
+    }
+#pragma unroll
+    for (int i = 0; i < M; ++i) {
+      float t = v[0][N + i];
+#pragma unroll
+      for (int w = 1; w < T / 64; ++w) t = fmaxf(t, v[w][N + i]);
+      most[i] = t;
+    }
   }
-  const float ref = ref_of(st.m), log_z = logf(z);
-  float kl = 0.0f;
+};
+
+// ---- what the teacher listed for a row, an entry or a few a thread
+
+__device__ inline float weight_of(const Args &g, uint64_t r) { return g.a.weight ? uniform_load(g.a.weight + r) : 1.0f; }
+
+constexpr uint32_t kOneWaveK = 256;   // most entries of rows that one wave handles (three registers an entry)
+
+template <int DT, int T>
+struct Listed {
+  static constexpr int PER = T == 64 ? (int)kOneWaveK / 64 : (int)kMaxLogitsK / T;   // entries a thread, at most
+  static constexpr uint32_t kNone = 0xffffffffu;
+  uint32_t n;            // entries of the record
+  uint32_t idx[PER];     // kNone: no entry, or one of no word
+  float val[PER], s[PER];  // the teacher's value, the student's logit
+  uint32_t label;        // kNone: no hard term
+  float s_label;
+  float rest;
+
+  // of the words [lo, hi) only (of every word the sums over a row need, of a stretch what its gradient needs)
+  template <bool HARD>
+  __device__ void read(const Args &g, const Row<DT> &row, uint64_t r, uint32_t lo, uint32_t hi) {
+    const Record rec(g.a.messages, r, g.a.message_stride, g.a.k, g.a.half);
+    n = rec.count(g.a.k);
+    rest = g.a.rest_too ? rec.rest() : 0.0f;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const uint32_t e = threadIdx.x + i * T;
+      idx[i] = kNone;
+      if (e < g.a.k) {   // (the record has room for k entries: read before n is known)
+        const uint32_t j = rec.idx(e);
+        val[i] = rec.val(e);
+        idx[i] = e < n && j >= lo && j < hi ? j : kNone;
+      }
+    }
+    label = kNone;
+    if (HARD) {
+      const int64_t l = g.a.labels[r];
+      if (l >= 0 && l < (int64_t)g.a.vocab) label = (uint32_t)l;
+    }
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+      if (idx[i] != kNone) s[i] = Num<DT>::get(row.p + idx[i]);
+    // (not of another stretch, whose gradient may just be written over it)
+    s_label = label != kNone && label >= lo && label < hi ? Num<DT>::get(row.p + label) : 0.0f;
+  }
+  // Marks the words of the vectors [v0, v1); barriers inside.
+  __device__ void mark(const Row<DT> &row, uint32_t v0, uint32_t v1, uint32_t *bits) const {
+    constexpr int E = Num<DT>::E;
+    for (uint32_t w = threadIdx.x; w < ((v1 - v0) * E + 31) / 32; w += T) bits[w] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const uint32_t at = idx[i] + row.off - v0 * E;   // (from the first word of vector v0)
+      if (idx[i] != kNone && idx[i] + row.off >= v0 * E && at < (v1 - v0) * E) atomicOr(&bits[at >> 5], 1u << (at & 31));
+    }
+    __syncthreads();
+  }
+};
+
+template <int T>
+struct FinishLds {
+  Exchange<T, 0, 2> most;
+  Exchange<T, 5, 0> sums;
+  Exchange<T, 1, 0> kl;
+};
+
+__device__ inline bool far(float m, float c2, bool two) {
+  return m != kNegInf && !(fabsf(m) * fmaxf(c2, two ? kLog2e : 0.0f) < kFarRef);
+}
+
+// A thread's sums over the vectors [v0, v1) relative to the largest logit m of all threads.
+template <int DT, bool TWO, int T>
+__device__ Part settled(FastSum f, float m, const Row<DT> &row, uint32_t v0, uint32_t v1, const Marks<DT> &marks, float c2) {
+  if (far(m, c2, TWO)) {
+    PlainSum q = scan_plain<DT, TWO, T>(row, v0, v1, marks, c2);
+    q.template move_to<TWO>(m, c2);
+    return q;
+  }
+  f.template move_to<TWO>(m, c2);
+  f.template settle<TWO>(c2);
+  return f;
+}
+
+// The row's loss and statistics from the sums of its unlisted words (TAIL_DROP: of all words), each thread's own.
+// HARD: 0 no hard term, 1 at the same temperature as the soft one, 2 at its own.  settle(m): a thread's sums relative
+// to m, the largest unlisted logit of all (0 where that is -inf).
+template <int DT, int HARD, int T, class Settle>
+__device__ Stats finish(const Args &g, const Listed<DT, T> &list, float largest, const Settle &settle, float weight, float *loss,
+                        FinishLds<T> &lds) {
+  constexpr int PER = Listed<DT, T>::PER;
+  constexpr bool TWO = HARD == 2;
+  const bool rest_too = g.a.rest_too;
+  float most[2] = {largest, kNegInf};
+#pragma unroll
+  for (int i = 0; i < PER; ++i)
+    if (list.idx[i] != list.kNone) most[1] = fmaxf(most[1], list.s[i]);
+  lds.most.all(nullptr, most);
+  const Part p = settle(most[0]);
+  // (TAIL_DROP: the listed words are in the sums already)
+  const float m = rest_too ? fmaxf(most[0], most[1]) : most[0], ref = ref_of(m);
+  float sums[5] = {p.s, TWO ? p.h : 0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    if (list.idx[i] == list.kNone) continue;
+    sums[2] += exp2_hw(list.val[i] * g.c2);
+    if (rest_too) {
+      const float d = list.s[i] - ref;
+      sums[3] += exp2_hw(d * g.c2);
+      if (TWO) sums[4] += exp2_hw(d * kLog2e);
+    }
+  }
+  lds.sums.all(sums, nullptr);
+  const float q = list.n == 0 ? 0.0f : sums[2] + list.rest;
+  const float down = ref_of(most[0]) - ref;   // from the reference of the unlisted words to that of the row
+  const float scale = most[0] == kNegInf ? 0.0f : exp2_hw(down * g.c2), scale1 = most[0] == kNegInf ? 0.0f : exp2_hw(down * kLog2e);
+  // (nothing unlisted: the sums are 0 whatever the scale)
+  const float z = (rest_too ? sums[0] * scale : sums[0]) + sums[3];
+  const float h = TWO ? (rest_too ? sums[1] * scale1 : sums[1]) + sums[4] : z;
+  const float log_z = logf(z);
+  float kl[1] = {0.0f};
   if (q != 0.0f) {
     const float log_q = logf(q);
-    for (uint32_t e = threadIdx.x; e < n; e += THREADS) {
-      const uint32_t j = rec.idx(e);
-      if (j >= g.a.vocab) continue;
-      const float val = rec.val(e), w = exp2_hw(val * g.c2) / q;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      if (list.idx[i] == list.kNone) continue;
+      const float w = exp2_hw(list.val[i] * g.c2) / q;
       // log(q_i / p_i); a word that the teacher gives nothing counts nothing, whatever the student gives it
-      if (w != 0.0f) kl += w * ((val - (Num<DT>::get(row.p + j) - ref)) * g.c + (log_z - log_q));
+      if (w != 0.0f) kl[0] += w * ((list.val[i] - (list.s[i] - ref)) * g.c + (log_z - log_q));
     }
-    kl = all_sum<THREADS>(kl, lds);
-    const float qr = rest / q;
-    if (rest_too && qr != 0.0f) kl += qr * (logf(qr) - ((p.m - ref) * g.c + logf(p.s) - log_z));
   }
+  lds.kl.all(kl, nullptr);
+  Stats st;
+  st.m = m;
+  st.m_r = most[0];
   st.inv_z = 1.0f / z;
   st.inv_h = 1.0f / h;
   st.inv_q = q != 0.0f ? 1.0f / q : 0.0f;
-  const float down = (ref_of(p.m) - ref) * 1.0f;
-  st.c_soft = exp2_hw(down * g.c2) * st.inv_z;
-  if (rest_too && rest != 0.0f && p.s != 0.0f) st.c_soft -= rest * st.inv_q / p.s;
-  st.c_hard = HARD == 0 ? 0.0f : exp2_hw(down * kLog2e) * st.inv_h;
+  st.c_soft = scale * st.inv_z;
+  const float q_r = q != 0.0f ? list.rest / q : 0.0f;
+  if (q_r != 0.0f && sums[0] != 0.0f) st.c_soft -= q_r / sums[0];
+  st.c_hard = HARD == 0 ? 0.0f : scale1 * st.inv_h;
   st.pad = 0.0f;
   if (loss && threadIdx.x == 0) {
-    float l = g.a.soft * kl;
-    uint32_t label;
-    if (HARD && hard_label(g, r, &label)) l += g.a.hard * (logf(h) - (Num<DT>::get(row.p + label) - ref));
-    *loss = weight == 0.0f ? 0.0f : weight * l;
+    if (q_r != 0.0f) kl[0] += q_r * (logf(q_r) - ((most[0] - ref) * g.c + logf(sums[0]) - log_z));
+    float l = g.a.soft * kl[0];
+    if (HARD && list.label != list.kNone) l += g.a.hard * (logf(h) - (list.s_label - ref));
+    *loss = weight * l;
   }
   return st;
 }
 
-// Gradient of the vectors [v0, v1) of a row.
-template <int DT, int HARD, int THREADS>
-__device__ void gradient(const Args &g, const Row<DT> &row, uint64_t r, uint32_t v0, uint32_t v1, float weight, const Stats &st) {
-  constexpr int E = Num<DT>::E;
-  using raw = typename Num<DT>::raw;
-  raw *out = reinterpret_cast<raw *>(g.a.grad) + uniform_off(r * g.a.grad_stride);
-  uint32_t b0, b1, label = 0xffffffffu;
-  row.body(v0, v1, &b0, &b1);
-  const bool hard = HARD && hard_label(g, r, &label);
-  const float soft = st.inv_q != 0.0f ? weight * g.a.soft * g.c : 0.0f;
-  const float ks = soft * st.c_soft, kh = hard ? weight * g.a.hard * st.c_hard : 0.0f;
-  const float ref = ref_of(st.m_r);
-  // the listed words of this stretch are read before anything is written (the gradient may lie over the logits)
-  const Record rec(g.a.messages, r, g.a.message_stride, g.a.k, g.a.half);
-  const uint32_t n = rec.count(g.a.k);
-  const uint32_t lo = v0 * E > row.off ? v0 * E - row.off : 0, hi = v1 * E - row.off < g.a.vocab ? v1 * E - row.off : g.a.vocab;
-  constexpr int PER = (kMaxLogitsK + THREADS - 1) / THREADS;
-  float kept[PER];
-  uint32_t at[PER];
-  bool label_listed = false;
-  const float ref_all = ref_of(st.m);
-#pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const uint32_t e = threadIdx.x + i * THREADS;
-    at[i] = 0xffffffffu;
-    if (weight == 0.0f || e >= n) continue;
-    const uint32_t j = rec.idx(e);
-    if (j < lo || j >= hi) continue;
-    at[i] = j;
-    const float d = Num<DT>::get(row.p + j) - ref_all;
-    float x = soft * (exp2_hw(d * g.c2) * st.inv_z - exp2_hw(rec.val(e) * g.c2) * st.inv_q);
-    if (hard) x += weight * g.a.hard * (exp2_hw(d * kLog2e) * st.inv_h - (j == label ? 1.0f : 0.0f));
-    if (j == label) label_listed = true;
-    kept[i] = x;
-  }
-  float at_label = 0.0f;
-  const bool mine = hard && weight != 0.0f && label >= lo && label < hi;
-  if (mine) {
-    const float d = Num<DT>::get(row.p + label) - ref;
-    at_label = ks * exp2_hw(d * g.c2) + kh * exp2_hw(d * kLog2e) - weight * g.a.hard;
-  }
-  label_listed = __syncthreads_or(label_listed);
-  const auto one = [&](float *x) {
+// ---- gradient of the vectors [v0, v1) of a row
+
+// What makes a gradient of an unlisted word's logit.
+struct Slope {
+  float c2, soft, hard, ref2, ref1;   // fast: soft * 2^(x c2 - ref2) + hard * 2^(x log2e - ref1)
+  float m;                            // plain: soft * 2^((x - m) c2) + ...
+  bool far_;
+  template <int HARD, int E>
+  __device__ void fast(float *x) const {
 #pragma unroll
     for (int i = 0; i < E; ++i) {
-      const float d = x[i] - ref;
-      float y = (HARD == 1 ? ks + kh : ks) * exp2_hw(d * g.c2);
-      if (HARD == 2) y += kh * exp2_hw(d * kLog2e);
-      x[i] = weight == 0.0f ? 0.0f : y;
+      float y = soft * base2_exp(x[i], c2, ref2);
+      if (HARD == 2) y = __builtin_fmaf(hard, base2_exp(x[i], kLog2e, ref1), y);
+      x[i] = y;
     }
-  };
-  for (uint32_t v = b0 + threadIdx.x; v < b1; v += THREADS) {
-    float x[E];
-    if (weight != 0.0f) Num<DT>::widen(row.load(v), x);
-    one(x);
-    const u32x4 y = Num<DT>::narrow(x);
-    __builtin_memcpy(out + ((int)(v * E) - (int)row.off), &y, 16);   // (grad may be aligned otherwise than the logits)
   }
-  const bool first = b0 > v0, last = b1 < v1;
-  if ((threadIdx.x == 0 && first) || (threadIdx.x == 1 && last)) {
-    const uint32_t v = threadIdx.x == 0 ? v0 : v1 - 1;
-    float x[E];
-    if (weight != 0.0f) row.load_any(v, x);
-    one(x);
+  template <int HARD, int E>
+  __device__ void plain(float *x) const {
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      const float d = x[i] - m;
+      float y = soft * exp2_hw(d * c2);
+      if (HARD == 2) y = __builtin_fmaf(hard, exp2_hw(d * kLog2e), y);
+      x[i] = y;
+    }
+  }
+};
+
+template <int DT, int HARD, int T>
+struct Gradient {
+  using raw = typename Num<DT>::raw;
+  static constexpr int E = Num<DT>::E, PER = Listed<DT, T>::PER;
+  const Row<DT> &row;
+  raw *out;
+  uint32_t v0, v1, b0, b1;
+  Slope k;
+  __device__ Gradient(const Args &g, const Row<DT> &row_, uint64_t r, uint32_t v0_, uint32_t v1_)
+      : row(row_), out(reinterpret_cast<raw *>(g.a.grad) + uniform_off(r * g.a.grad_stride)), v0(v0_), v1(v1_) {
+    row.body(v0, v1, &b0, &b1);
+  }
+  // (the gradient may be aligned otherwise than the logits)
+  __device__ void put(uint32_t v, u32x4 y) const {
+    __builtin_nontemporal_store(y, reinterpret_cast<u32x4_any *>(out + ((int)(v * E) - (int)row.off)));
+  }
+  __device__ void put_any(uint32_t v, const float *x) const {
 #pragma unroll
     for (int i = 0; i < E; ++i) {
       const int j = (int)(v * E) - (int)row.off + i;
-      if (j >= 0 && j < (int)g.a.vocab) Num<DT>::put(out + j, x[i]);
+      if (j >= 0 && j < (int)row.vocab) Num<DT>::put(out + j, x[i]);
     }
   }
-  __syncthreads();   // the words below were written by other threads, too
+  __device__ bool edge(uint32_t *v) const {
+    *v = threadIdx.x == 0 ? v0 : v1 - 1;
+    return (threadIdx.x == 0 && b0 > v0) || (threadIdx.x == 1 && b1 < v1);
+  }
+  __device__ void zero() const {
+    const u32x4 none = {0, 0, 0, 0};
+    for (uint32_t v = b0 + threadIdx.x; v < b1; v += T) put(v, none);
+    const float x[E] = {};
+    uint32_t v;
+    if (edge(&v)) put_any(v, x);
+  }
+  // The slope; listed words' gradients take the place of their logits, the label's that of its own.
+  __device__ void prepare(const Args &g, float weight, const Stats &st, Listed<DT, T> &list) {
+    const float soft = st.inv_q != 0.0f ? weight * g.a.soft * g.c : 0.0f;
+    const float hard = list.label != list.kNone ? weight * g.a.hard : 0.0f;
+    const float ref = ref_of(st.m);
+    k.c2 = g.c2;
+    k.m = ref_of(st.m_r);
+    k.far_ = far(st.m_r, g.c2, HARD == 2);
+    k.soft = soft * st.c_soft;
+    k.hard = hard * st.c_hard;
+    if (list.label != list.kNone) {
+      const float d = list.s_label - k.m;
+      list.s_label = k.soft * exp2_hw(d * g.c2) + (HARD ? k.hard * exp2_hw(d * kLog2e) : 0.0f) - hard;
+    }
+    if (HARD == 1) k.soft += k.hard;
+    k.ref2 = base2_ref(st.m_r, g.c2);
+    k.ref1 = base2_ref(st.m_r, kLog2e);
+    if (!k.far_ && st.m_r != kNegInf) {
+      // (nothing else has to change: a coefficient takes up the rounding of the reference)
+      if (k.soft != 0.0f) k.soft *= exp2_hw(-__builtin_fmaf(st.m_r, g.c2, -k.ref2));
+      if (k.hard != 0.0f) k.hard *= exp2_hw(-__builtin_fmaf(st.m_r, kLog2e, -k.ref1));
+    }
 #pragma unroll
-  for (int i = 0; i < PER; ++i)
-    if (at[i] != 0xffffffffu) Num<DT>::put(out + at[i], kept[i]);
-  if (mine && !label_listed && threadIdx.x == 0) Num<DT>::put(out + label, at_label);
+    for (int i = 0; i < PER; ++i) {
+      if (list.idx[i] == list.kNone) continue;
+      const float d = list.s[i] - ref;
+      float x = soft * (exp2_hw(d * g.c2) * st.inv_z - exp2_hw(list.val[i] * g.c2) * st.inv_q);
+      if (HARD && hard != 0.0f) x += hard * (exp2_hw(d * kLog2e) * st.inv_h - (list.idx[i] == list.label ? 1.0f : 0.0f));
+      list.s[i] = x;
+    }
+  }
+  __device__ void one(float *x) const {
+    if (k.far_) k.template plain<HARD, E>(x);
+    else k.template fast<HARD, E>(x);
+  }
+  __device__ void edges() const {
+    uint32_t v;
+    if (edge(&v)) {
+      float x[E];
+      row.load_any(v, x);
+      one(x);
+      put_any(v, x);
+    }
+  }
+  // The whole vectors, read again.
+  __device__ void stream() const {
+    if (k.far_) {
+      for (uint32_t v = b0 + threadIdx.x; v < b1; v += T) {
+        float x[E];
+        Num<DT>::widen(row.load(v), x);
+        k.template plain<HARD, E>(x);
+        put(v, Num<DT>::narrow(x));
+      }
+      return;
+    }
+    uint32_t v = b0 + threadIdx.x;
+    for (uint32_t all = (b1 - b0) / (4 * T); all > 0; --all, v += 4 * T) {
+      u32x4 w[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) w[u] = row.load(v + u * T);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        float x[E];
+        Num<DT>::widen(w[u], x);
+        k.template fast<HARD, E>(x);
+        put(v + u * T, Num<DT>::narrow(x));
+      }
+    }
+    for (; v < b1; v += T) {
+      float x[E];
+      Num<DT>::widen(row.load(v), x);
+      k.template fast<HARD, E>(x);
+      put(v, Num<DT>::narrow(x));
+    }
+  }
+  // The listed words and the label, after the others: those were written by other threads, too.
+  __device__ void listed(const Args &g, const Listed<DT, T> &list) const {
+    bool label_listed = false;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) label_listed = label_listed || (list.idx[i] != list.kNone && list.idx[i] == list.label);
+    label_listed = __syncthreads_or(label_listed);
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+      if (list.idx[i] != list.kNone) Num<DT>::put(out + list.idx[i], list.s[i]);
+    const uint32_t lo = v0 * E > row.off ? v0 * E - row.off : 0, hi = v1 * E - row.off < row.vocab ? v1 * E - row.off : row.vocab;
+    if (HARD && list.label >= lo && list.label < hi && !label_listed && threadIdx.x == 0) Num<DT>::put(out + list.label, list.s_label);
+  }
+};
+
+// ---- kernels
+
+__device__ inline void put_stats(const Args &g, uint64_t r, const Stats &st) {
+  if (g.a.stats && threadIdx.x == 0) reinterpret_cast<Stats *>(g.a.stats)[r] = st;
 }
 
-__device__ inline float weight_of(const Args &g, uint64_t r) { return g.a.weight ? uniform_load(g.a.weight + r) : 1.0f; }
+// Whole rows, a workgroup each: the loss.
+template <int DT, int HARD, int T, uint32_t MOST>
+__global__ __launch_bounds__(T) void distill_loss_kernel(Args g) {
+  __shared__ uint32_t bits[MOST * Num<DT>::E / 32];
+  __shared__ FinishLds<T> lds;
+  const uint64_t r = blockIdx.x;
+  const float weight = weight_of(g, r);
+  if (weight == 0.0f) {
+    if (threadIdx.x == 0) g.a.loss[r] = 0.0f;
+    put_stats(g, r, Stats{});
+    return;
+  }
+  const Row<DT> row(g.a.logits, r, g.a.row_stride, g.a.vocab);
+  Listed<DT, T> list;
+  list.template read<HARD != 0>(g, row, r, 0, row.vocab);
+  if (g.a.rest_too) list.mark(row, 0, row.nv, bits);
+  const Marks<DT> marks{g.a.rest_too ? (const uint8_t *)bits : nullptr, 0};
+  const FastSum f = scan<DT, HARD == 2, T>(row, 0, row.nv, marks, g.c2);
+  const auto settle = [&](float m) { return settled<DT, HARD == 2, T>(f, m, row, 0, row.nv, marks, g.c2); };
+  const Stats st = finish<DT, HARD, T>(g, list, f.m, settle, weight, g.a.loss + r, lds);
+  put_stats(g, r, st);
+}
 
-// Whole rows, a workgroup each: the loss and, with STEP, the gradient.
-template <int DT, int HARD, int THREADS, bool STEP>
-__global__ __launch_bounds__(THREADS) void distill_rows_kernel(Args g) {
-  __shared__ uint32_t bits[kChunkVecs * Num<DT>::E / 32];
-  __shared__ float lds[THREADS / 64];
+// Whole rows, a workgroup each, loss and gradient: the row stays in registers, HOLD vectors a thread.
+template <int DT, int HARD, int T, int HOLD, int WAVES>
+__global__ __launch_bounds__(T, WAVES) void distill_step_kernel(Args g) {
+  constexpr int E = Num<DT>::E;
+  constexpr bool TWO = HARD == 2;
+  __shared__ uint32_t bits[(T * HOLD + 2) * E / 32 + 1];   // (whole vectors and two partial ones)
+  __shared__ FinishLds<T> lds;
   const uint64_t r = blockIdx.x;
   const Row<DT> row(g.a.logits, r, g.a.row_stride, g.a.vocab);
   const float weight = weight_of(g, r);
-  Stats st{};
-  if (weight != 0.0f) {
-    if (g.a.rest_too) mark<DT, THREADS>(g, row, r, 0, row.nv, bits);
-    const Part p = scan<DT, HARD == 2, THREADS>(row, 0, row.nv, g.a.rest_too, Marks<DT>{(const uint8_t *)bits, 0}, g.c2, lds);
-    st = finish<DT, HARD, THREADS>(g, row, r, p, weight, g.a.loss + r, lds);
-  } else if (threadIdx.x == 0) {
-    g.a.loss[r] = 0.0f;
+  Gradient<DT, HARD, T> grad(g, row, r, 0, row.nv);
+  if (weight == 0.0f) {
+    if (threadIdx.x == 0) g.a.loss[r] = 0.0f;
+    grad.zero();
+    return;
   }
-  if (g.a.stats && threadIdx.x == 0) reinterpret_cast<Stats *>(g.a.stats)[r] = st;
-  if (STEP) gradient<DT, HARD, THREADS>(g, row, r, 0, row.nv, weight, st);
+  const uint32_t b0 = grad.b0, b1 = grad.b1;
+  u32x4 w[HOLD];
+#pragma unroll
+  for (int i = 0; i < HOLD; ++i) {
+    const uint32_t v = b0 + i * T + threadIdx.x;
+    w[i] = Num<DT>::masked();
+    if (v < b1) w[i] = row.load(v);
+  }
+  Listed<DT, T> list;
+  list.template read<HARD != 0>(g, row, r, 0, row.vocab);
+  if (g.a.rest_too) list.mark(row, 0, row.nv, bits);
+  const Marks<DT> marks{g.a.rest_too ? (const uint8_t *)bits : nullptr, 0};
+  // largest unlisted logit; from here on the listed ones are -inf here (their gradients are written apart)
+  float largest = kNegInf;
+#pragma unroll
+  for (int i = 0; i < HOLD; ++i) {
+    const uint32_t v = b0 + i * T + threadIdx.x;
+    if (b0 + i * T < b1) {   // (uniform)
+      float x[E];
+      Num<DT>::widen(w[i], x);
+      if (g.a.rest_too && v < b1 && marks.apply(v, x)) w[i] = Num<DT>::narrow(x);
+#pragma unroll
+      for (int e = 0; e < E; ++e) largest = fmaxf(largest, x[e]);
+    }
+  }
+  float ends[E];
+  uint32_t end_v;
+  const bool has_end = grad.edge(&end_v);
+  if (has_end) {
+    row.load_any(end_v, ends);
+    marks.apply(end_v, ends);
+#pragma unroll
+    for (int e = 0; e < E; ++e) largest = fmaxf(largest, ends[e]);
+  }
+  const auto settle = [&](float m) -> Part {
+    if (far(m, g.c2, TWO)) {
+      PlainSum q = scan_plain<DT, TWO, T>(row, 0, row.nv, marks, g.c2);
+      q.template move_to<TWO>(m, g.c2);
+      return q;
+    }
+    FastSum f;
+    f.m = m;
+    const float ref = base2_ref(m, g.c2), ref1 = base2_ref(m, kLog2e);
+    const auto add = [&](const float *x) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        f.s += base2_exp(x[e], g.c2, ref);
+        if (TWO) f.h += base2_exp(x[e], kLog2e, ref1);
+      }
+    };
+#pragma unroll
+    for (int i = 0; i < HOLD; ++i) {
+      if (b0 + i * T < b1) {
+        float x[E];
+        Num<DT>::widen(w[i], x);
+        add(x);
+      }
+    }
+    if (has_end) add(ends);
+    f.template settle<TWO>(g.c2);
+    return f;
+  };
+  const Stats st = finish<DT, HARD, T>(g, list, largest, settle, weight, g.a.loss + r, lds);
+  grad.prepare(g, weight, st, list);
+  if (grad.k.far_) {
+    grad.stream();
+  } else {
+#pragma unroll
+    for (int i = 0; i < HOLD; ++i) {
+      const uint32_t v = b0 + i * T + threadIdx.x;
+      if (v < b1) {
+        float x[E];
+        Num<DT>::widen(w[i], x);
+        grad.k.template fast<HARD, E>(x);
+        grad.put(v, Num<DT>::narrow(x));
+      }
+    }
+  }
+  grad.edges();
+  grad.listed(g, list);
 }
 
-// Sums of one chunk of a row.
-template <int DT, int HARD, int THREADS>
-__global__ __launch_bounds__(THREADS) void distill_scan_kernel(Args g, float *partial) {
+// Rows that one workgroup cannot hold: sums of chunks, loss and statistics from those, gradients of chunks.  (Gradients
+// wait for a launch of their own, because they may be written over listed logits that other chunks' losses need.)
+constexpr int kChunkThreads = 256;
+
+template <int DT, int HARD>
+__global__ __launch_bounds__(kChunkThreads) void distill_scan_kernel(Args g, float *partial) {
+  constexpr int T = kChunkThreads;
+  constexpr bool TWO = HARD == 2;
   __shared__ uint32_t bits[kChunkVecs * Num<DT>::E / 32];
-  __shared__ float lds[THREADS / 64];
+  __shared__ Exchange<T, 0, 1> most;
+  __shared__ Exchange<T, 2, 0> sums;
   const uint64_t r = blockIdx.x;
+  if (weight_of(g, r) == 0.0f) return;
   const Row<DT> row(g.a.logits, r, g.a.row_stride, g.a.vocab);
   const uint32_t v0 = blockIdx.y * g.vecs < row.nv ? blockIdx.y * g.vecs : row.nv;
   const uint32_t v1 = v0 + g.vecs < row.nv ? v0 + g.vecs : row.nv;
-  Part p;
-  if (weight_of(g, r) != 0.0f) {
-    if (g.a.rest_too) mark<DT, THREADS>(g, row, r, v0, v1, bits);
-    p = scan<DT, HARD == 2, THREADS>(row, v0, v1, g.a.rest_too, Marks<DT>{(const uint8_t *)bits, v0}, g.c2, lds);
+  if (g.a.rest_too) {
+    Listed<DT, T> list;
+    list.template read<false>(g, row, r, 0, row.vocab);
+    list.mark(row, v0, v1, bits);
   }
+  const Marks<DT> marks{g.a.rest_too ? (const uint8_t *)bits : nullptr, v0};
+  const FastSum f = scan<DT, TWO, T>(row, v0, v1, marks, g.c2);
+  float m[1] = {f.m};
+  most.all(nullptr, m);
+  const Part p = settled<DT, TWO, T>(f, m[0], row, v0, v1, marks, g.c2);
+  float s[2] = {p.s, TWO ? p.h : 0.0f};
+  sums.all(s, nullptr);
   if (threadIdx.x == 0) {
     float *o = partial + (r * g.chunks + blockIdx.y) * kPartialFloats;
-    o[0] = p.m;
-    o[1] = p.s;
-    o[2] = p.h;
+    o[0] = m[0];
+    o[1] = s[0];
+    o[2] = s[1];
   }
 }
 
-template <int DT, int HARD, int THREADS>
-__global__ __launch_bounds__(THREADS) void distill_finish_kernel(Args g, const float *partial) {
-  __shared__ float lds[THREADS / 64];
+// Loss and statistics of a row from its chunks' sums.
+template <int DT, int HARD>
+__global__ __launch_bounds__(kChunkThreads) void distill_join_kernel(Args g, const float *partial) {
+  constexpr int T = kChunkThreads;
+  constexpr bool TWO = HARD == 2;
+  __shared__ FinishLds<T> lds;
   const uint64_t r = blockIdx.x;
-  const Row<DT> row(g.a.logits, r, g.a.row_stride, g.a.vocab);
   const float weight = weight_of(g, r);
-  Stats st{};
-  if (weight != 0.0f) {
-    Part p;
-    for (uint32_t i = threadIdx.x; i < g.chunks; i += THREADS) {
-      const float *o = partial + (r * g.chunks + i) * kPartialFloats;
-      Part x;
-      x.m = o[0]; x.s = o[1]; x.h = o[2];
-      const float nm = fmaxf(p.m, x.m);
-      p.rescale<HARD == 2>(nm, g.c2);
-      x.rescale<HARD == 2>(nm, g.c2);
-      p.s += x.s;
-      p.h += x.h;
-    }
-    p.rescale<HARD == 2>(all_max<THREADS>(p.m, lds), g.c2);
-    p.s = all_sum<THREADS>(p.s, lds);
-    if (HARD == 2) p.h = all_sum<THREADS>(p.h, lds);
-    st = finish<DT, HARD, THREADS>(g, row, r, p, weight, g.a.loss + r, lds);
-  } else if (threadIdx.x == 0) {
-    g.a.loss[r] = 0.0f;
+  if (weight == 0.0f) {
+    if (threadIdx.x == 0) g.a.loss[r] = 0.0f;
+    put_stats(g, r, Stats{});
+    return;
   }
-  if (g.a.stats && threadIdx.x == 0) reinterpret_cast<Stats *>(g.a.stats)[r] = st;
+  const Row<DT> row(g.a.logits, r, g.a.row_stride, g.a.vocab);
+  Listed<DT, T> list;
+  list.template read<HARD != 0>(g, row, r, 0, row.vocab);
+  PlainSum p;
+  for (uint32_t i = threadIdx.x; i < g.chunks; i += T) {
+    const float *o = partial + (r * g.chunks + i) * kPartialFloats;
+    PlainSum x;
+    x.m = o[0];
+    x.s = o[1];
+    x.h = o[2];
+    const float nm = fmaxf(p.m, x.m);
+    p.template move_to<TWO>(nm, g.c2);
+    x.template move_to<TWO>(nm, g.c2);
+    p.s += x.s;
+    p.h += x.h;
+  }
+  const auto settle = [&](float m) {
+    PlainSum q = p;
+    q.template move_to<TWO>(m, g.c2);
+    return q;
+  };
+  put_stats(g, r, finish<DT, HARD, T>(g, list, p.m, settle, weight, g.a.loss + r, lds));
 }
 
-template <int DT, int HARD, int THREADS>
-__global__ __launch_bounds__(THREADS) void distill_grad_kernel(Args g) {
+template <int DT, int HARD>
+__global__ __launch_bounds__(kChunkThreads) void distill_grad_kernel(Args g) {
+  constexpr int E = Num<DT>::E;
   const uint64_t r = blockIdx.x;
   const Row<DT> row(g.a.logits, r, g.a.row_stride, g.a.vocab);
-  const uint32_t v0 = blockIdx.y * g.vecs < row.nv ? blockIdx.y * g.vecs : row.nv;
-  const uint32_t v1 = v0 + g.vecs < row.nv ? v0 + g.vecs : row.nv;
+  const uint32_t v0 = blockIdx.y * g.vecs, v1 = v0 + g.vecs < row.nv ? v0 + g.vecs : row.nv;
   if (v0 >= v1) return;
-  gradient<DT, HARD, THREADS>(g, row, r, v0, v1, weight_of(g, r), reinterpret_cast<const Stats *>(g.a.stats)[r]);
+  const float weight = weight_of(g, r);
+  Gradient<DT, HARD, kChunkThreads> grad(g, row, r, v0, v1);
+  if (weight == 0.0f) {
+    grad.zero();
+    return;
+  }
+  Listed<DT, kChunkThreads> list;
+  const uint32_t lo = v0 * E > row.off ? v0 * E - row.off : 0, hi = v1 * E - row.off < row.vocab ? v1 * E - row.off : row.vocab;
+  list.template read<HARD != 0>(g, row, r, lo, hi);
+  grad.prepare(g, weight, reinterpret_cast<const Stats *>(g.a.stats)[r], list);
+  // every thread has read the listed logits of its entries before any is written over
+  __syncthreads();
+  grad.stream();
+  grad.edges();
+  grad.listed(g, list);
 }
 
-constexpr int kRowThreads = 256;
+template <int DT, int HARD, int T, int HOLD, int WAVES>
+static hipError_t step_rows(const Args &g, hipStream_t stream) {
+  distill_step_kernel<DT, HARD, T, HOLD, WAVES><<<(uint32_t)g.a.rows, T, 0, stream>>>(g);
+  return hipGetLastError();
+}
 
 template <int DT, int HARD>
 static hipError_t run_typed(Args g, DistillRole role, uint8_t *ws, hipStream_t stream) {
-  const uint32_t rows = (uint32_t)g.a.rows;
+  const uint32_t rows = (uint32_t)g.a.rows, nv = row_vecs(g.a.vocab, DT, g.a.row_stride);
   const Cut cut = cut_rows(g.a.rows, g.a.vocab, DT, g.a.row_stride);
-  g.chunks = cut.chunks;
-  g.vecs = cut.vecs;
-  const DistillWs lay = distill_ws(g.a.rows, cut);
-  const dim3 grid(rows, cut.chunks);
-  if (role == DistillRole::grad) {
-    distill_grad_kernel<DT, HARD, kRowThreads><<<grid, kRowThreads, 0, stream>>>(g);
+  if (role == DistillRole::loss && cut.chunks == 1) {
+    if (nv <= 1024 && g.a.k <= kOneWaveK) distill_loss_kernel<DT, HARD, 64, 1024><<<rows, 64, 0, stream>>>(g);
+    else if (rows >= 1024) distill_loss_kernel<DT, HARD, 256, kChunkVecs><<<rows, 256, 0, stream>>>(g);
+    else distill_loss_kernel<DT, HARD, 1024, kChunkVecs><<<rows, 1024, 0, stream>>>(g);
     return hipGetLastError();
   }
-  if (cut.chunks == 1) {
-    if (role == DistillRole::loss) distill_rows_kernel<DT, HARD, kRowThreads, false><<<rows, kRowThreads, 0, stream>>>(g);
-    else distill_rows_kernel<DT, HARD, kRowThreads, true><<<rows, kRowThreads, 0, stream>>>(g);
-    return hipGetLastError();
+  if (role == DistillRole::step && cut.chunks == 1) {
+    if (nv <= 512 && g.a.k <= kOneWaveK) return step_rows<DT, HARD, 64, 8, 4>(g, stream);
+    if (nv <= 2048) return step_rows<DT, HARD, 256, 8, 5>(g, stream);
+    if (nv <= 4096) return step_rows<DT, HARD, 256, 16, 4>(g, stream);
+    if (nv <= 8192) return step_rows<DT, HARD, 512, 16, 4>(g, stream);
+    return step_rows<DT, HARD, 1024, 16, 4>(g, stream);
   }
-  float *partial = reinterpret_cast<float *>(ws + lay.partial);
-  if (!g.a.stats) g.a.stats = ws + lay.stats;
-  distill_scan_kernel<DT, HARD, kRowThreads><<<grid, kRowThreads, 0, stream>>>(g, partial);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  distill_finish_kernel<DT, HARD, kRowThreads><<<rows, kRowThreads, 0, stream>>>(g, partial);
-  e = hipGetLastError();
-  if (e != hipSuccess || role == DistillRole::loss) return e;
-  distill_grad_kernel<DT, HARD, kRowThreads><<<grid, kRowThreads, 0, stream>>>(g);
+  if (role != DistillRole::grad) {
+    const DistillWs lay = distill_ws(g.a.rows, cut);
+    float *partial = reinterpret_cast<float *>(ws + lay.partial);
+    if (!g.a.stats) g.a.stats = ws + lay.stats;
+    g.chunks = cut.chunks;
+    g.vecs = cut.vecs;
+    distill_scan_kernel<DT, HARD><<<dim3(rows, cut.chunks), kChunkThreads, 0, stream>>>(g, partial);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    distill_join_kernel<DT, HARD><<<rows, kChunkThreads, 0, stream>>>(g, partial);
+    e = hipGetLastError();
+    if (e != hipSuccess || role == DistillRole::loss) return e;
+  }
+  g.vecs = kGradVecs;
+  distill_grad_kernel<DT, HARD><<<dim3(rows, (uint32_t)cdiv(nv, kGradVecs)), kChunkThreads, 0, stream>>>(g);
   return hipGetLastError();
 }
 

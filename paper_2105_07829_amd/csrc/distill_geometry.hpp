@@ -36,6 +36,8 @@ inline uint32_t row_vecs(uint32_t vocab, int dtype, uint64_t row_stride) {
   return (uint32_t)cdiv(vocab + (row_stride % e ? e - 1 : 0), e);
 }
 
+constexpr uint32_t kGradVecs = 4096;   // vectors of a row whose gradient one workgroup writes
+
 // Rows are cut into chunks, a workgroup each, where one workgroup may not have them whole.
 struct Cut {
   uint32_t chunks;   // a row

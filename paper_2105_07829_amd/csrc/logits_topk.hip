@@ -188,17 +188,6 @@ struct Tally {
 
 constexpr int kTopThreads = 256;
 
-// What exponents of base 2 are taken relative to: the largest logit times c2, as f32 rounds it.  Any reference will
-// do as long as all parties to a sum know it, so the rounding costs nothing, and x * c2 - reference is one
-// instruction, with one rounding.  Below -2^20 (masked by -inf or by a type's lowest value) it stays there: 2^x is 0
-// next to any row that is handled so.
-constexpr float kLowRef = -0x1p20f;
-__device__ inline float base2_ref(float m, float c2) { return fmaxf(m * c2, kLowRef); }
-__device__ inline float base2_exp(float x, float c2, float ref2) { return exp2_hw(__builtin_fmaf(x, c2, -ref2)); }
-// Rows whose largest logit is further from 0 than this (or NaN, or infinite) go the other way: the rounding of the
-// reference would be felt.
-constexpr float kFarRef = 0x1p16f;
-
 // Rows by groups.  One pass finds every group's largest logit and its sum of exponentials (relative to that logit); at
 // least k logits reach the k-th largest of the groups' largest (or a little less), so only the few groups that reach
 // it are looked through again for candidates.  A thread loads four vectors at a time, kTopThreads apart; PER of them
