@@ -389,7 +389,8 @@ bpc_status_t bpc_adaptive_update(const bpc_params_t *params,
  *     the loss is +inf and the gradient of the listed words still -q_i.
  *   - A NaN or +inf among a row's logits makes that row's loss and gradient NaN.
  * Unlike the gradient path these calls take infinities and NaN as described.  Sums are
- * formed in f32 in a fixed order: the same inputs give the same bits.
+ * formed in f32 in a fixed order: the same inputs give the same bits (in rows that start
+ * elsewhere in their 128-byte line, or of another number, sums may be formed in another order).
  * Limits (BPC_ERR_UNSUPPORTED beyond): vocab <= 2^24, k <= BPC_LOGITS_MAX_K (k may exceed
  * vocab), rows < 2^22.  rows == 0 is a no-op returning BPC_OK.
  */

@@ -36,7 +36,7 @@ inline uint32_t row_vecs(uint32_t vocab, int dtype, uint64_t row_stride) {
   return (uint32_t)cdiv(vocab + (row_stride % e ? e - 1 : 0), e);
 }
 
-constexpr uint32_t kGradVecs = 4096;   // vectors of a row whose gradient one workgroup writes
+constexpr uint32_t kGradVecs = 16384;   // vectors of a row whose gradient one workgroup writes
 
 // Rows are cut into chunks, a workgroup each, where one workgroup may not have them whole.
 struct Cut {
@@ -45,10 +45,9 @@ struct Cut {
 };
 inline Cut cut_rows(uint64_t rows, uint32_t vocab, int dtype, uint64_t row_stride) {
   (void)rows;
-  const uint32_t nv = row_vecs(vocab, dtype, row_stride);
   Cut c;
-  c.chunks = (uint32_t)cdiv(nv, kChunkVecs);
-  c.vecs = (uint32_t)cdiv(nv, c.chunks);
+  c.chunks = (uint32_t)cdiv(row_vecs(vocab, dtype, row_stride), kChunkVecs);
+  c.vecs = (uint32_t)cdiv(row_vecs(vocab, dtype, row_stride), c.chunks);
   return c;
 }
 

@@ -10,6 +10,7 @@
 // and the pass takes the whole row).  The gradient of an unlisted word is
 //   w exp((s_j - m_R) c) a c [exp((m_R - m) c) / Z - q_R / R] + w b exp(s_j - m_R) exp(m_R - m) / H,
 // two coefficients a row; the listed words and the label are written apart, after the others.
+#pragma once
 #include "distill.hpp"
 #include "kernels.hpp"
 
@@ -41,24 +42,47 @@ struct Marks {
   static constexpr int E = Num<DT>::E;
   const uint8_t *bits;   // NULL: nothing is marked
   uint32_t v0;
-  __device__ bool apply(uint32_t v, float *x) const {   // marked words count as masked; whether there are any
-    if (!bits) return false;
+  __device__ uint32_t of(uint32_t v) const {
     const uint32_t i = v - v0;
-    const uint32_t b = E == 8 ? bits[i] : (bits[i >> 1] >> (4 * (i & 1))) & 15u;
-    if (b) {
+    return E == 8 ? bits[i] : (bits[i >> 1] >> (4 * (i & 1))) & 15u;
+  }
+  // Marked words count as masked.  N vectors, `apart` apart, from v on; whether any word is marked.
+  template <int N>
+  __device__ bool apply(uint32_t v, uint32_t apart, float *x) const {
+    if (!bits) return false;
+    uint32_t b[N], any = 0;
 #pragma unroll
-      for (int k = 0; k < E; ++k) x[k] = (b >> k) & 1 ? kNegInf : x[k];
+    for (int u = 0; u < N; ++u) any |= b[u] = of(v + u * apart);
+    if (any) {
+#pragma unroll
+      for (int u = 0; u < N; ++u)
+#pragma unroll
+        for (int k = 0; k < E; ++k) x[u * E + k] = (b[u] >> k) & 1 ? kNegInf : x[u * E + k];
     }
-    return b != 0;
+    return any != 0;
   }
 };
 
 // ---- sums over a stretch of a row, each thread its own
 
-// With references of base 2 (see base2_ref).  TWO: at temperature 1, too.
+// The hard term of a call, which is at temperature 1: none; at the soft one's temperature; at its own; or at its own
+// where that of the soft one is 2 or 4, so that its exponentials are the second and fourth powers of the soft one's
+// (a product or two instead of a multiply-add and an exponential).
+enum Hard { kNoHard, kSameHard, kOwnHard, kSquareHard, kFourthHard };
+constexpr bool two_sums(int hard) { return hard >= kOwnHard; }
+// 2^(x log2e - ref1) from e = 2^(x c2 - ref2) (ref1 = 2 ref2 or 4 ref2 where that is what it takes).
+template <int HARD>
+__device__ inline float hard_exp(float x, float e, float ref1) {
+  if (HARD == kSquareHard) return e * e;
+  if (HARD == kFourthHard) return (e * e) * (e * e);
+  return base2_exp(x, kLog2e, ref1);
+}
+
+// With references of base 2 (see base2_ref).
 struct FastSum : Part {
-  template <bool TWO, int N>
+  template <int HARD, int N>
   __device__ void add(const float *x, float c2) {
+    constexpr bool TWO = two_sums(HARD);
     float nm = m;
 #pragma unroll
     for (int i = 0; i < N; ++i) nm = fmaxf(nm, x[i]);
@@ -68,8 +92,9 @@ struct FastSum : Part {
     m = nm;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      s += base2_exp(x[i], c2, ref);
-      if (TWO) h += base2_exp(x[i], kLog2e, ref1);
+      const float e = base2_exp(x[i], c2, ref);
+      s += e;
+      if (TWO) h += hard_exp<HARD>(x[i], e, ref1);
     }
   }
   // relative to the largest of all threads' instead
@@ -96,8 +121,9 @@ struct PlainSum : Part {
     if (TWO) h *= exp2_hw(d * kLog2e);
     m = nm;
   }
-  template <bool TWO, int N>
+  template <int HARD, int N>
   __device__ void add(const float *x, float c2) {
+    constexpr bool TWO = two_sums(HARD);
     float nm = m;
 #pragma unroll
     for (int i = 0; i < N; ++i) nm = fmaxf(nm, x[i]);
@@ -112,60 +138,75 @@ struct PlainSum : Part {
   }
 };
 
-// The partial vectors at the ends of the stretch [v0, v1) whose whole vectors are [b0, b1): one thread each.
-template <int DT, bool TWO, class Sum>
-__device__ void add_edges(const Row<DT> &row, uint32_t v0, uint32_t v1, uint32_t b0, uint32_t b1, const Marks<DT> &marks, float c2, Sum *p) {
-  if ((threadIdx.x == 0 && b0 > v0) || (threadIdx.x == 1 && b1 < v1)) {
-    const uint32_t v = threadIdx.x == 0 ? v0 : v1 - 1;
+// The vectors beside a stretch's body.
+template <int DT, int HARD, class Sum>
+__device__ void add_edges(const Row<DT> &row, const Stretch &st, const Marks<DT> &marks, float c2, Sum *p) {
+  uint32_t v;
+  if (st.edge(&v)) {
     float x[Num<DT>::E];
     row.load_any(v, x);
-    marks.apply(v, x);
-    p->template add<TWO, Num<DT>::E>(x, c2);
+    marks.template apply<1>(v, 0, x);
+    p->template add<HARD, Num<DT>::E>(x, c2);
   }
 }
 
-// A thread's share of the vectors [v0, v1): four loads at a time.
-template <int DT, bool TWO, int T>
-__device__ FastSum scan(const Row<DT> &row, uint32_t v0, uint32_t v1, const Marks<DT> &marks, float c2) {
+// Four vectors of a body a thread, T apart, from v on; what is past its end reads as masked.
+template <int DT, int T>
+struct Four {
+  u32x4 w[4];
+  __device__ void load(const Row<DT> &row, const Stretch &st, uint32_t v) {
+    if (v + 4 * T <= st.b1) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) w[u] = row.load_once(v + u * T, threadIdx.x);
+    } else {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        w[u] = Num<DT>::masked();
+        if (v + u * T + threadIdx.x < st.b1) w[u] = row.load_once(v + u * T, threadIdx.x);
+      }
+    }
+  }
+};
+
+// A thread's share of a stretch; `now`: the first four vectors, loaded by the caller before whatever else a row needs.
+template <int DT, int HARD, int T>
+__device__ FastSum scan(const Row<DT> &row, const Stretch &st, Four<DT, T> now, const Marks<DT> &marks, float c2) {
   constexpr int E = Num<DT>::E;
   FastSum p;
-  uint32_t b0, b1;
-  row.body(v0, v1, &b0, &b1);
-  uint32_t v = b0 + threadIdx.x;
-  for (uint32_t all = (b1 - b0) / (4 * T); all > 0; --all, v += 4 * T) {
-    u32x4 w[4];
-#pragma unroll
-    for (int u = 0; u < 4; ++u) w[u] = row.load(v + u * T);
+  uint32_t v = st.b0;
+  while (v + 4 * T <= st.b1) {
     float x[4 * E];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      Num<DT>::widen(w[u], x + u * E);
-      marks.apply(v + u * T, x + u * E);
+    for (int u = 0; u < 4; ++u) Num<DT>::widen(now.w[u], x + u * E);
+    const uint32_t at = v;
+    v += 4 * T;
+    if (v < st.b1) now.load(row, st, v);   // (the next four are on their way)
+    marks.template apply<4>(at + threadIdx.x, T, x);
+    p.add<HARD, 4 * E>(x, c2);
+  }
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    if (v + u * T + threadIdx.x < st.b1) {
+      float x[E];
+      Num<DT>::widen(now.w[u], x);
+      marks.template apply<1>(v + u * T + threadIdx.x, 0, x);
+      p.add<HARD, E>(x, c2);
     }
-    p.add<TWO, 4 * E>(x, c2);
   }
-  for (; v < b1; v += T) {
-    float x[E];
-    Num<DT>::widen(row.load(v), x);
-    marks.apply(v, x);
-    p.add<TWO, E>(x, c2);
-  }
-  add_edges<DT, TWO>(row, v0, v1, b0, b1, marks, c2, &p);
+  add_edges<DT, HARD>(row, st, marks, c2, &p);
   return p;
 }
-template <int DT, bool TWO, int T>
-__device__ PlainSum scan_plain(const Row<DT> &row, uint32_t v0, uint32_t v1, const Marks<DT> &marks, float c2) {
+template <int DT, int HARD, int T>
+__device__ PlainSum scan_plain(const Row<DT> &row, const Stretch &st, const Marks<DT> &marks, float c2) {
   constexpr int E = Num<DT>::E;
   PlainSum p;
-  uint32_t b0, b1;
-  row.body(v0, v1, &b0, &b1);
-  for (uint32_t v = b0 + threadIdx.x; v < b1; v += T) {
+  for (uint32_t v = st.b0 + threadIdx.x; v < st.b1; v += T) {
     float x[E];
-    Num<DT>::widen(row.load(v), x);
-    marks.apply(v, x);
-    p.add<TWO, E>(x, c2);
+    Num<DT>::widen(row.load(0, v), x);
+    marks.template apply<1>(v, 0, x);
+    p.add<HARD, E>(x, c2);
   }
-  add_edges<DT, TWO>(row, v0, v1, b0, b1, marks, c2, &p);
+  add_edges<DT, HARD>(row, st, marks, c2, &p);
   return p;
 }
 
@@ -275,11 +316,12 @@ __device__ inline bool far(float m, float c2, bool two) {
   return m != kNegInf && !(fabsf(m) * fmaxf(c2, two ? kLog2e : 0.0f) < kFarRef);
 }
 
-// A thread's sums over the vectors [v0, v1) relative to the largest logit m of all threads.
-template <int DT, bool TWO, int T>
-__device__ Part settled(FastSum f, float m, const Row<DT> &row, uint32_t v0, uint32_t v1, const Marks<DT> &marks, float c2) {
+// A thread's sums over a stretch relative to the largest logit m of all threads.
+template <int DT, int HARD, int T>
+__device__ Part settled(FastSum f, float m, const Row<DT> &row, const Stretch &st, const Marks<DT> &marks, float c2) {
+  constexpr bool TWO = two_sums(HARD);
   if (far(m, c2, TWO)) {
-    PlainSum q = scan_plain<DT, TWO, T>(row, v0, v1, marks, c2);
+    PlainSum q = scan_plain<DT, HARD, T>(row, st, marks, c2);
     q.template move_to<TWO>(m, c2);
     return q;
   }
@@ -289,13 +331,13 @@ __device__ Part settled(FastSum f, float m, const Row<DT> &row, uint32_t v0, uin
 }
 
 // The row's loss and statistics from the sums of its unlisted words (TAIL_DROP: of all words), each thread's own.
-// HARD: 0 no hard term, 1 at the same temperature as the soft one, 2 at its own.  settle(m): a thread's sums relative
+// settle(m): a thread's sums relative
 // to m, the largest unlisted logit of all (0 where that is -inf).
 template <int DT, int HARD, int T, class Settle>
 __device__ Stats finish(const Args &g, const Listed<DT, T> &list, float largest, const Settle &settle, float weight, float *loss,
                         FinishLds<T> &lds) {
   constexpr int PER = Listed<DT, T>::PER;
-  constexpr bool TWO = HARD == 2;
+  constexpr bool TWO = two_sums(HARD);
   const bool rest_too = g.a.rest_too;
   float most[2] = {largest, kNegInf};
 #pragma unroll
@@ -345,7 +387,7 @@ __device__ Stats finish(const Args &g, const Listed<DT, T> &list, float largest,
   st.c_soft = scale * st.inv_z;
   const float q_r = q != 0.0f ? list.rest / q : 0.0f;
   if (q_r != 0.0f && sums[0] != 0.0f) st.c_soft -= q_r / sums[0];
-  st.c_hard = HARD == 0 ? 0.0f : scale1 * st.inv_h;
+  st.c_hard = HARD == kNoHard ? 0.0f : scale1 * st.inv_h;
   st.pad = 0.0f;
   if (loss && threadIdx.x == 0) {
     if (q_r != 0.0f) kl[0] += q_r * (logf(q_r) - ((most[0] - ref) * g.c + logf(sums[0]) - log_z));
@@ -356,7 +398,7 @@ __device__ Stats finish(const Args &g, const Listed<DT, T> &list, float largest,
   return st;
 }
 
-// ---- gradient of the vectors [v0, v1) of a row
+// ---- gradient of a stretch of a row
 
 // What makes a gradient of an unlisted word's logit.
 struct Slope {
@@ -367,8 +409,9 @@ struct Slope {
   __device__ void fast(float *x) const {
 #pragma unroll
     for (int i = 0; i < E; ++i) {
-      float y = soft * base2_exp(x[i], c2, ref2);
-      if (HARD == 2) y = __builtin_fmaf(hard, base2_exp(x[i], kLog2e, ref1), y);
+      const float e = base2_exp(x[i], c2, ref2);
+      float y = soft * e;
+      if (two_sums(HARD)) y = __builtin_fmaf(hard, hard_exp<HARD>(x[i], e, ref1), y);
       x[i] = y;
     }
   }
@@ -378,7 +421,7 @@ struct Slope {
     for (int i = 0; i < E; ++i) {
       const float d = x[i] - m;
       float y = soft * exp2_hw(d * c2);
-      if (HARD == 2) y = __builtin_fmaf(hard, exp2_hw(d * kLog2e), y);
+      if (two_sums(HARD)) y = __builtin_fmaf(hard, exp2_hw(d * kLog2e), y);
       x[i] = y;
     }
   }
@@ -390,15 +433,15 @@ struct Gradient {
   static constexpr int E = Num<DT>::E, PER = Listed<DT, T>::PER;
   const Row<DT> &row;
   raw *out;
-  uint32_t v0, v1, b0, b1;
+  Stretch st;
   Slope k;
   __device__ Gradient(const Args &g, const Row<DT> &row_, uint64_t r, uint32_t v0_, uint32_t v1_)
-      : row(row_), out(reinterpret_cast<raw *>(g.a.grad) + uniform_off(r * g.a.grad_stride)), v0(v0_), v1(v1_) {
-    row.body(v0, v1, &b0, &b1);
-  }
+      : row(row_), out(reinterpret_cast<raw *>(g.a.grad) + uniform_off(r * g.a.grad_stride)), st(row_, v0_, v1_) {}
   // (the gradient may be aligned otherwise than the logits)
-  __device__ void put(uint32_t v, u32x4 y) const {
-    __builtin_nontemporal_store(y, reinterpret_cast<u32x4_any *>(out + ((int)(v * E) - (int)row.off)));
+  __device__ void put(int v, u32x4 y) const {   // vector v + threadIdx.x, v the same in every lane
+    uint8_t *at = reinterpret_cast<uint8_t *>(out) + ((int64_t)v * 16 - (int64_t)(row.off * sizeof(raw)));
+    // (past the caches: nothing here reads it again; loss and gradient of 4096 rows of 50,257 bf16 270 us without, 223 so)
+    __builtin_nontemporal_store(y, reinterpret_cast<u32x4_any *>(at + threadIdx.x * 16u));
   }
   __device__ void put_any(uint32_t v, const float *x) const {
 #pragma unroll
@@ -407,45 +450,42 @@ struct Gradient {
       if (j >= 0 && j < (int)row.vocab) Num<DT>::put(out + j, x[i]);
     }
   }
-  __device__ bool edge(uint32_t *v) const {
-    *v = threadIdx.x == 0 ? v0 : v1 - 1;
-    return (threadIdx.x == 0 && b0 > v0) || (threadIdx.x == 1 && b1 < v1);
-  }
   __device__ void zero() const {
     const u32x4 none = {0, 0, 0, 0};
-    for (uint32_t v = b0 + threadIdx.x; v < b1; v += T) put(v, none);
+    for (uint32_t v = st.b0; v < st.b1; v += T)
+      if (v + threadIdx.x < st.b1) put(v, none);
     const float x[E] = {};
     uint32_t v;
-    if (edge(&v)) put_any(v, x);
+    if (st.edge(&v)) put_any(v, x);
   }
   // The slope; listed words' gradients take the place of their logits, the label's that of its own.
-  __device__ void prepare(const Args &g, float weight, const Stats &st, Listed<DT, T> &list) {
-    const float soft = st.inv_q != 0.0f ? weight * g.a.soft * g.c : 0.0f;
+  __device__ void prepare(const Args &g, float weight, const Stats &stats, Listed<DT, T> &list) {
+    const float soft = stats.inv_q != 0.0f ? weight * g.a.soft * g.c : 0.0f;
     const float hard = list.label != list.kNone ? weight * g.a.hard : 0.0f;
-    const float ref = ref_of(st.m);
+    const float ref = ref_of(stats.m);
     k.c2 = g.c2;
-    k.m = ref_of(st.m_r);
-    k.far_ = far(st.m_r, g.c2, HARD == 2);
-    k.soft = soft * st.c_soft;
-    k.hard = hard * st.c_hard;
+    k.m = ref_of(stats.m_r);
+    k.far_ = far(stats.m_r, g.c2, two_sums(HARD));
+    k.soft = soft * stats.c_soft;
+    k.hard = hard * stats.c_hard;
     if (list.label != list.kNone) {
       const float d = list.s_label - k.m;
       list.s_label = k.soft * exp2_hw(d * g.c2) + (HARD ? k.hard * exp2_hw(d * kLog2e) : 0.0f) - hard;
     }
-    if (HARD == 1) k.soft += k.hard;
-    k.ref2 = base2_ref(st.m_r, g.c2);
-    k.ref1 = base2_ref(st.m_r, kLog2e);
-    if (!k.far_ && st.m_r != kNegInf) {
+    if (HARD == kSameHard) k.soft += k.hard;
+    k.ref2 = base2_ref(stats.m_r, g.c2);
+    k.ref1 = base2_ref(stats.m_r, kLog2e);
+    if (!k.far_ && stats.m_r != kNegInf) {
       // (nothing else has to change: a coefficient takes up the rounding of the reference)
-      if (k.soft != 0.0f) k.soft *= exp2_hw(-__builtin_fmaf(st.m_r, g.c2, -k.ref2));
-      if (k.hard != 0.0f) k.hard *= exp2_hw(-__builtin_fmaf(st.m_r, kLog2e, -k.ref1));
+      if (k.soft != 0.0f) k.soft *= exp2_hw(-__builtin_fmaf(stats.m_r, g.c2, -k.ref2));
+      if (k.hard != 0.0f) k.hard *= exp2_hw(-__builtin_fmaf(stats.m_r, kLog2e, -k.ref1));
     }
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       if (list.idx[i] == list.kNone) continue;
       const float d = list.s[i] - ref;
-      float x = soft * (exp2_hw(d * g.c2) * st.inv_z - exp2_hw(list.val[i] * g.c2) * st.inv_q);
-      if (HARD && hard != 0.0f) x += hard * (exp2_hw(d * kLog2e) * st.inv_h - (list.idx[i] == list.label ? 1.0f : 0.0f));
+      float x = soft * (exp2_hw(d * g.c2) * stats.inv_z - exp2_hw(list.val[i] * g.c2) * stats.inv_q);
+      if (HARD && hard != 0.0f) x += hard * (exp2_hw(d * kLog2e) * stats.inv_h - (list.idx[i] == list.label ? 1.0f : 0.0f));
       list.s[i] = x;
     }
   }
@@ -455,42 +495,39 @@ struct Gradient {
   }
   __device__ void edges() const {
     uint32_t v;
-    if (edge(&v)) {
+    if (st.edge(&v)) {
       float x[E];
       row.load_any(v, x);
       one(x);
       put_any(v, x);
     }
   }
-  // The whole vectors, read again.
-  __device__ void stream() const {
+  // The body; `now`: its first four vectors.
+  __device__ void stream(Four<DT, T> now) const {
     if (k.far_) {
-      for (uint32_t v = b0 + threadIdx.x; v < b1; v += T) {
-        float x[E];
-        Num<DT>::widen(row.load(v), x);
-        k.template plain<HARD, E>(x);
-        put(v, Num<DT>::narrow(x));
+      for (uint32_t v = st.b0; v < st.b1; v += T) {
+        if (v + threadIdx.x < st.b1) {
+          float x[E];
+          Num<DT>::widen(row.load(v, threadIdx.x), x);
+          k.template plain<HARD, E>(x);
+          put(v, Num<DT>::narrow(x));
+        }
       }
       return;
     }
-    uint32_t v = b0 + threadIdx.x;
-    for (uint32_t all = (b1 - b0) / (4 * T); all > 0; --all, v += 4 * T) {
-      u32x4 w[4];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) w[u] = row.load(v + u * T);
+    for (uint32_t v = st.b0; v < st.b1; v += 4 * T) {
+      Four<DT, T> next;
+      if (v + 4 * T < st.b1) next.load(row, st, v + 4 * T);
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
-        float x[E];
-        Num<DT>::widen(w[u], x);
-        k.template fast<HARD, E>(x);
-        put(v + u * T, Num<DT>::narrow(x));
+        if (v + u * T + threadIdx.x < st.b1) {
+          float x[E];
+          Num<DT>::widen(now.w[u], x);
+          k.template fast<HARD, E>(x);
+          put(v + u * T, Num<DT>::narrow(x));
+        }
       }
-    }
-    for (; v < b1; v += T) {
-      float x[E];
-      Num<DT>::widen(row.load(v), x);
-      k.template fast<HARD, E>(x);
-      put(v, Num<DT>::narrow(x));
+      now = next;
     }
   }
   // The listed words and the label, after the others: those were written by other threads, too.
@@ -502,7 +539,7 @@ struct Gradient {
 #pragma unroll
     for (int i = 0; i < PER; ++i)
       if (list.idx[i] != list.kNone) Num<DT>::put(out + list.idx[i], list.s[i]);
-    const uint32_t lo = v0 * E > row.off ? v0 * E - row.off : 0, hi = v1 * E - row.off < row.vocab ? v1 * E - row.off : row.vocab;
+    const uint32_t lo = st.v0 * E > row.off ? st.v0 * E - row.off : 0, hi = st.v1 * E - row.off < row.vocab ? st.v1 * E - row.off : row.vocab;
     if (HARD && list.label >= lo && list.label < hi && !label_listed && threadIdx.x == 0) Num<DT>::put(out + list.label, list.s_label);
   }
 };
@@ -526,21 +563,25 @@ __global__ __launch_bounds__(T) void distill_loss_kernel(Args g) {
     return;
   }
   const Row<DT> row(g.a.logits, r, g.a.row_stride, g.a.vocab);
+  const Stretch whole(row, 0, row.nv);
+  Four<DT, T> first;
+  first.load(row, whole, whole.b0);
   Listed<DT, T> list;
-  list.template read<HARD != 0>(g, row, r, 0, row.vocab);
+  list.template read<HARD != kNoHard>(g, row, r, 0, row.vocab);
   if (g.a.rest_too) list.mark(row, 0, row.nv, bits);
   const Marks<DT> marks{g.a.rest_too ? (const uint8_t *)bits : nullptr, 0};
-  const FastSum f = scan<DT, HARD == 2, T>(row, 0, row.nv, marks, g.c2);
-  const auto settle = [&](float m) { return settled<DT, HARD == 2, T>(f, m, row, 0, row.nv, marks, g.c2); };
+  const FastSum f = scan<DT, HARD, T>(row, whole, first, marks, g.c2);
+  const auto settle = [&](float m) { return settled<DT, HARD, T>(f, m, row, whole, marks, g.c2); };
   const Stats st = finish<DT, HARD, T>(g, list, f.m, settle, weight, g.a.loss + r, lds);
   put_stats(g, r, st);
 }
 
-// Whole rows, a workgroup each, loss and gradient: the row stays in registers, HOLD vectors a thread.
+// Whole rows, a workgroup each, loss and gradient: the row stays in registers, HOLD vectors a thread, all of them
+// requested before anything else.
 template <int DT, int HARD, int T, int HOLD, int WAVES>
-__global__ __launch_bounds__(T, WAVES) void distill_step_kernel(Args g) {
+__global__ __launch_bounds__(T, WAVES) void distill_held_kernel(Args g) {
   constexpr int E = Num<DT>::E;
-  constexpr bool TWO = HARD == 2;
+  constexpr bool TWO = two_sums(HARD);
   __shared__ uint32_t bits[(T * HOLD + 2) * E / 32 + 1];   // (whole vectors and two partial ones)
   __shared__ FinishLds<T> lds;
   const uint64_t r = blockIdx.x;
@@ -552,16 +593,20 @@ __global__ __launch_bounds__(T, WAVES) void distill_step_kernel(Args g) {
     grad.zero();
     return;
   }
-  const uint32_t b0 = grad.b0, b1 = grad.b1;
+  const uint32_t b0 = grad.st.b0, b1 = grad.st.b1;
   u32x4 w[HOLD];
 #pragma unroll
   for (int i = 0; i < HOLD; ++i) {
-    const uint32_t v = b0 + i * T + threadIdx.x;
-    w[i] = Num<DT>::masked();
-    if (v < b1) w[i] = row.load(v);
+    const uint32_t v = b0 + i * T;
+    if (v + T <= b1) {   // (uniform)
+      w[i] = row.load_once(v, threadIdx.x);
+    } else {
+      w[i] = Num<DT>::masked();
+      if (v + threadIdx.x < b1) w[i] = row.load_once(v, threadIdx.x);
+    }
   }
   Listed<DT, T> list;
-  list.template read<HARD != 0>(g, row, r, 0, row.vocab);
+  list.template read<HARD != kNoHard>(g, row, r, 0, row.vocab);
   if (g.a.rest_too) list.mark(row, 0, row.nv, bits);
   const Marks<DT> marks{g.a.rest_too ? (const uint8_t *)bits : nullptr, 0};
   // largest unlisted logit; from here on the listed ones are -inf here (their gradients are written apart)
@@ -569,26 +614,26 @@ __global__ __launch_bounds__(T, WAVES) void distill_step_kernel(Args g) {
 #pragma unroll
   for (int i = 0; i < HOLD; ++i) {
     const uint32_t v = b0 + i * T + threadIdx.x;
-    if (b0 + i * T < b1) {   // (uniform)
+    if (b0 + i * T < b1) {
       float x[E];
       Num<DT>::widen(w[i], x);
-      if (g.a.rest_too && v < b1 && marks.apply(v, x)) w[i] = Num<DT>::narrow(x);
+      if (v < b1 && marks.template apply<1>(v, 0, x)) w[i] = Num<DT>::narrow(x);
 #pragma unroll
       for (int e = 0; e < E; ++e) largest = fmaxf(largest, x[e]);
     }
   }
   float ends[E];
   uint32_t end_v;
-  const bool has_end = grad.edge(&end_v);
+  const bool has_end = grad.st.edge(&end_v);
   if (has_end) {
     row.load_any(end_v, ends);
-    marks.apply(end_v, ends);
+    marks.template apply<1>(end_v, 0, ends);
 #pragma unroll
     for (int e = 0; e < E; ++e) largest = fmaxf(largest, ends[e]);
   }
   const auto settle = [&](float m) -> Part {
     if (far(m, g.c2, TWO)) {
-      PlainSum q = scan_plain<DT, TWO, T>(row, 0, row.nv, marks, g.c2);
+      PlainSum q = scan_plain<DT, HARD, T>(row, grad.st, marks, g.c2);
       q.template move_to<TWO>(m, g.c2);
       return q;
     }
@@ -598,8 +643,9 @@ __global__ __launch_bounds__(T, WAVES) void distill_step_kernel(Args g) {
     const auto add = [&](const float *x) {
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        f.s += base2_exp(x[e], g.c2, ref);
-        if (TWO) f.h += base2_exp(x[e], kLog2e, ref1);
+        const float y = base2_exp(x[e], g.c2, ref);
+        f.s += y;
+        if (TWO) f.h += hard_exp<HARD>(x[e], y, ref1);
       }
     };
 #pragma unroll
@@ -617,12 +663,12 @@ __global__ __launch_bounds__(T, WAVES) void distill_step_kernel(Args g) {
   const Stats st = finish<DT, HARD, T>(g, list, largest, settle, weight, g.a.loss + r, lds);
   grad.prepare(g, weight, st, list);
   if (grad.k.far_) {
-    grad.stream();
+    grad.stream(Four<DT, T>{});
   } else {
 #pragma unroll
     for (int i = 0; i < HOLD; ++i) {
-      const uint32_t v = b0 + i * T + threadIdx.x;
-      if (v < b1) {
+      const uint32_t v = b0 + i * T;
+      if (v + threadIdx.x < b1) {
         float x[E];
         Num<DT>::widen(w[i], x);
         grad.k.template fast<HARD, E>(x);
@@ -641,7 +687,7 @@ constexpr int kChunkThreads = 256;
 template <int DT, int HARD>
 __global__ __launch_bounds__(kChunkThreads) void distill_scan_kernel(Args g, float *partial) {
   constexpr int T = kChunkThreads;
-  constexpr bool TWO = HARD == 2;
+  constexpr bool TWO = two_sums(HARD);
   __shared__ uint32_t bits[kChunkVecs * Num<DT>::E / 32];
   __shared__ Exchange<T, 0, 1> most;
   __shared__ Exchange<T, 2, 0> sums;
@@ -650,16 +696,19 @@ __global__ __launch_bounds__(kChunkThreads) void distill_scan_kernel(Args g, flo
   const Row<DT> row(g.a.logits, r, g.a.row_stride, g.a.vocab);
   const uint32_t v0 = blockIdx.y * g.vecs < row.nv ? blockIdx.y * g.vecs : row.nv;
   const uint32_t v1 = v0 + g.vecs < row.nv ? v0 + g.vecs : row.nv;
+  const Stretch chunk(row, v0, v1);
+  Four<DT, T> first;
+  first.load(row, chunk, chunk.b0);
   if (g.a.rest_too) {
     Listed<DT, T> list;
     list.template read<false>(g, row, r, 0, row.vocab);
     list.mark(row, v0, v1, bits);
   }
   const Marks<DT> marks{g.a.rest_too ? (const uint8_t *)bits : nullptr, v0};
-  const FastSum f = scan<DT, TWO, T>(row, v0, v1, marks, g.c2);
+  const FastSum f = scan<DT, HARD, T>(row, chunk, first, marks, g.c2);
   float m[1] = {f.m};
   most.all(nullptr, m);
-  const Part p = settled<DT, TWO, T>(f, m[0], row, v0, v1, marks, g.c2);
+  const Part p = settled<DT, HARD, T>(f, m[0], row, chunk, marks, g.c2);
   float s[2] = {p.s, TWO ? p.h : 0.0f};
   sums.all(s, nullptr);
   if (threadIdx.x == 0) {
@@ -674,7 +723,7 @@ __global__ __launch_bounds__(kChunkThreads) void distill_scan_kernel(Args g, flo
 template <int DT, int HARD>
 __global__ __launch_bounds__(kChunkThreads) void distill_join_kernel(Args g, const float *partial) {
   constexpr int T = kChunkThreads;
-  constexpr bool TWO = HARD == 2;
+  constexpr bool TWO = two_sums(HARD);
   __shared__ FinishLds<T> lds;
   const uint64_t r = blockIdx.x;
   const float weight = weight_of(g, r);
@@ -685,7 +734,7 @@ __global__ __launch_bounds__(kChunkThreads) void distill_join_kernel(Args g, con
   }
   const Row<DT> row(g.a.logits, r, g.a.row_stride, g.a.vocab);
   Listed<DT, T> list;
-  list.template read<HARD != 0>(g, row, r, 0, row.vocab);
+  list.template read<HARD != kNoHard>(g, row, r, 0, row.vocab);
   PlainSum p;
   for (uint32_t i = threadIdx.x; i < g.chunks; i += T) {
     const float *o = partial + (r * g.chunks + i) * kPartialFloats;
@@ -707,33 +756,36 @@ __global__ __launch_bounds__(kChunkThreads) void distill_join_kernel(Args g, con
   put_stats(g, r, finish<DT, HARD, T>(g, list, p.m, settle, weight, g.a.loss + r, lds));
 }
 
-template <int DT, int HARD>
-__global__ __launch_bounds__(kChunkThreads) void distill_grad_kernel(Args g) {
+// The gradient from statistics, a workgroup a row (or a stretch of kGradVecs vectors of it).
+template <int DT, int HARD, int T>
+__global__ __launch_bounds__(T) void distill_grad_kernel(Args g) {
   constexpr int E = Num<DT>::E;
   const uint64_t r = blockIdx.x;
   const Row<DT> row(g.a.logits, r, g.a.row_stride, g.a.vocab);
   const uint32_t v0 = blockIdx.y * g.vecs, v1 = v0 + g.vecs < row.nv ? v0 + g.vecs : row.nv;
   if (v0 >= v1) return;
   const float weight = weight_of(g, r);
-  Gradient<DT, HARD, kChunkThreads> grad(g, row, r, v0, v1);
+  Gradient<DT, HARD, T> grad(g, row, r, v0, v1);
   if (weight == 0.0f) {
     grad.zero();
     return;
   }
-  Listed<DT, kChunkThreads> list;
+  Four<DT, T> first;
+  first.load(row, grad.st, grad.st.b0);
+  Listed<DT, T> list;
   const uint32_t lo = v0 * E > row.off ? v0 * E - row.off : 0, hi = v1 * E - row.off < row.vocab ? v1 * E - row.off : row.vocab;
-  list.template read<HARD != 0>(g, row, r, lo, hi);
+  list.template read<HARD != kNoHard>(g, row, r, lo, hi);
   grad.prepare(g, weight, reinterpret_cast<const Stats *>(g.a.stats)[r], list);
   // every thread has read the listed logits of its entries before any is written over
   __syncthreads();
-  grad.stream();
+  grad.stream(first);
   grad.edges();
   grad.listed(g, list);
 }
 
 template <int DT, int HARD, int T, int HOLD, int WAVES>
-static hipError_t step_rows(const Args &g, hipStream_t stream) {
-  distill_step_kernel<DT, HARD, T, HOLD, WAVES><<<(uint32_t)g.a.rows, T, 0, stream>>>(g);
+static hipError_t held_rows(const Args &g, hipStream_t stream) {
+  distill_held_kernel<DT, HARD, T, HOLD, WAVES><<<(uint32_t)g.a.rows, T, 0, stream>>>(g);
   return hipGetLastError();
 }
 
@@ -748,11 +800,11 @@ static hipError_t run_typed(Args g, DistillRole role, uint8_t *ws, hipStream_t s
     return hipGetLastError();
   }
   if (role == DistillRole::step && cut.chunks == 1) {
-    if (nv <= 512 && g.a.k <= kOneWaveK) return step_rows<DT, HARD, 64, 8, 4>(g, stream);
-    if (nv <= 2048) return step_rows<DT, HARD, 256, 8, 5>(g, stream);
-    if (nv <= 4096) return step_rows<DT, HARD, 256, 16, 4>(g, stream);
-    if (nv <= 8192) return step_rows<DT, HARD, 512, 16, 4>(g, stream);
-    return step_rows<DT, HARD, 1024, 16, 4>(g, stream);
+    if (nv <= 512 && g.a.k <= kOneWaveK) return held_rows<DT, HARD, 64, 8, 4>(g, stream);
+    if (nv <= 2048) return held_rows<DT, HARD, 256, 8, 5>(g, stream);
+    if (nv <= 4096) return held_rows<DT, HARD, 256, 16, 4>(g, stream);
+    if (nv <= 8192) return held_rows<DT, HARD, 512, 16, 4>(g, stream);
+    return held_rows<DT, HARD, 1024, 16, 4>(g, stream);
   }
   if (role != DistillRole::grad) {
     const DistillWs lay = distill_ws(g.a.rows, cut);
@@ -767,28 +819,26 @@ static hipError_t run_typed(Args g, DistillRole role, uint8_t *ws, hipStream_t s
     e = hipGetLastError();
     if (e != hipSuccess || role == DistillRole::loss) return e;
   }
+  // (as many threads as a row keeps busy: the fewer rows are on their way at a time, the better the memory takes the
+  // writes; 4096 rows of 50,257 bf16, whose loss takes 68 us, 229 / 218 / 209 us for both with 256 / 512 / 1024)
   g.vecs = kGradVecs;
-  distill_grad_kernel<DT, HARD><<<dim3(rows, (uint32_t)cdiv(nv, kGradVecs)), kChunkThreads, 0, stream>>>(g);
+  const dim3 grid(rows, (uint32_t)cdiv(nv, kGradVecs));
+  if (nv <= 512) distill_grad_kernel<DT, HARD, 256><<<grid, 256, 0, stream>>>(g);
+  else distill_grad_kernel<DT, HARD, 1024><<<grid, 1024, 0, stream>>>(g);
   return hipGetLastError();
 }
 
 template <int DT>
-static hipError_t run_hard(const Args &g, DistillRole role, uint8_t *ws, hipStream_t stream) {
-  if (!g.a.labels || g.a.hard == 0.0f) return run_typed<DT, 0>(g, role, ws, stream);
-  if (g.c == 1.0f) return run_typed<DT, 1>(g, role, ws, stream);
-  return run_typed<DT, 2>(g, role, ws, stream);
-}
-
-hipError_t distill_run(const DistillCall &call, DistillRole role, uint8_t *ws, hipStream_t stream) {
+static hipError_t run_hard(const DistillCall &call, DistillRole role, uint8_t *ws, hipStream_t stream) {
   Args g{};
   g.a = call;
   g.c = 1.0f / call.temperature;
   g.c2 = (float)(1.44269504088896340736 / (double)call.temperature);
-  switch (call.dtype) {
-    case BPC_F32: return run_hard<BPC_F32>(g, role, ws, stream);
-    case BPC_F16: return run_hard<BPC_F16>(g, role, ws, stream);
-    default: return run_hard<BPC_BF16>(g, role, ws, stream);
-  }
+  if (!call.labels || call.hard == 0.0f) return run_typed<DT, kNoHard>(g, role, ws, stream);
+  if (call.temperature == 1.0f) return run_typed<DT, kSameHard>(g, role, ws, stream);
+  if (call.temperature == 2.0f) return run_typed<DT, kSquareHard>(g, role, ws, stream);
+  if (call.temperature == 4.0f) return run_typed<DT, kFourthHard>(g, role, ws, stream);
+  return run_typed<DT, kOwnHard>(g, role, ws, stream);
 }
 
 }  // namespace bpc

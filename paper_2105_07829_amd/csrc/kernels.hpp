@@ -141,7 +141,14 @@ struct DistillCall {
   uint64_t grad_stride;
 };
 enum class DistillRole { loss, grad, step };
-hipError_t distill_run(const DistillCall &call, DistillRole role, uint8_t *ws, hipStream_t stream);
+hipError_t distill_run_f32(const DistillCall &call, DistillRole role, uint8_t *ws, hipStream_t stream);
+hipError_t distill_run_f16(const DistillCall &call, DistillRole role, uint8_t *ws, hipStream_t stream);
+hipError_t distill_run_bf16(const DistillCall &call, DistillRole role, uint8_t *ws, hipStream_t stream);
+inline hipError_t distill_run(const DistillCall &call, DistillRole role, uint8_t *ws, hipStream_t stream) {
+  return call.dtype == BPC_F32 ? distill_run_f32(call, role, ws, stream)
+         : call.dtype == BPC_F16 ? distill_run_f16(call, role, ws, stream)
+                                 : distill_run_bf16(call, role, ws, stream);
+}
 hipError_t logits_topk(const DistillCall &call, uint8_t *out, uint8_t *ws, hipStream_t stream);
 
 }  // namespace bpc

@@ -193,7 +193,8 @@ constexpr int kTopThreads = 256;
 // it are looked through again for candidates.  A thread loads four vectors at a time, kTopThreads apart; PER of them
 // (1, 2, or 4 in each of 1 << shift such loads) make a group.
 template <int DT, int PER>
-__global__ __launch_bounds__(kTopThreads) void logits_topk_groups_kernel(TeacherArgs g, uint32_t shift, uint32_t n_groups, uint32_t cap) {
+__global__ __launch_bounds__(kTopThreads) void logits_topk_groups_kernel(TeacherArgs g, uint32_t shift, uint32_t n_groups, uint32_t cap,
+                                                                          uint32_t region) {
   constexpr int E = Num<DT>::E, T = kTopThreads, Q = 4 / PER;
   extern __shared__ __align__(16) uint8_t dyn[];
   __shared__ float lds[T / 64], lds_min[T / 64];
@@ -209,25 +210,24 @@ __global__ __launch_bounds__(kTopThreads) void logits_topk_groups_kernel(Teacher
   const Row<DT> row(g.a.logits, r, g.a.row_stride, g.a.vocab);
   uint32_t *gkey = reinterpret_cast<uint32_t *>(dyn);
   float *gsum = reinterpret_cast<float *>(gkey + n_groups);
-  uint32_t *ckey = reinterpret_cast<uint32_t *>(gsum + n_groups);
+  uint32_t *ckey = reinterpret_cast<uint32_t *>(dyn + region);
   uint32_t *cidx = ckey + cap;
   uint16_t *glist = reinterpret_cast<uint16_t *>(cidx + cap);
-  uint32_t b0, b1;
-  row.body(0, row.nv, &b0, &b1);
-  const uint32_t loads = (b1 - b0 + 4 * T - 1) / (4 * T), whole_loads = (b1 - b0) / (4 * T);
+  const Stretch all(row, 0, row.nv);
+  const uint32_t b0 = all.b0, b1 = all.b1, loads = (b1 - b0 + 4 * T - 1) / (4 * T);
   const float c2 = g.c2;
   float top = kNegInf;
   uint32_t done = 0;   // groups written
   float m = kNegInf, s = 0.0f;
   for (uint32_t b = 0; b < loads; ++b) {
     u32x4 w[4];
-    const uint32_t v0 = b0 + b * 4 * T + threadIdx.x;
-    if (b < whole_loads) {
+    const uint32_t v0 = b0 + b * 4 * T;
+    if (v0 + 4 * T <= b1) {
 #pragma unroll
-      for (int u = 0; u < 4; ++u) w[u] = row.load_cached(v0 + u * T);
+      for (int u = 0; u < 4; ++u) w[u] = row.load(v0 + u * T, threadIdx.x);
     } else {
 #pragma unroll
-      for (int u = 0; u < 4; ++u) w[u] = v0 + u * T < b1 ? row.load_cached(v0 + u * T) : Num<DT>::masked();
+      for (int u = 0; u < 4; ++u) w[u] = v0 + u * T + threadIdx.x < b1 ? row.load(v0 + u * T, threadIdx.x) : Num<DT>::masked();
     }
 #pragma unroll
     for (int q = 0; q < Q; ++q) {
@@ -259,10 +259,10 @@ __global__ __launch_bounds__(kTopThreads) void logits_topk_groups_kernel(Teacher
   }
   // every thread's largest logit is the largest of some groups: T of them reach the smallest of those
   float least = -wave_max(-top);
-  // the partial vectors at the ends are nobody's group: they are looked through in any case
+  // the vectors beside the body are nobody's group: they are looked through in any case
   float edge[E];
-  const bool has_edge = (threadIdx.x == 0 && b0 > 0) || (threadIdx.x == 1 && b1 < row.nv);
-  const uint32_t edge_v = threadIdx.x == 0 ? 0 : row.nv - 1;
+  uint32_t edge_v;
+  const bool has_edge = all.edge(&edge_v);
   bool odd = false;
   if (has_edge) {
     row.load_any(edge_v, edge);
@@ -344,7 +344,7 @@ __global__ __launch_bounds__(kTopThreads) void logits_topk_groups_kernel(Teacher
     const uint32_t v = b0 + (((id / T) << vg_shift) + u) * T + id % T;
     if (v < b1) {
       float x[E];
-      Num<DT>::widen(row.load_cached(v), x);
+      Num<DT>::widen(row.load(0, v), x);
       look(x, v * E - row.off);
     }
   }
@@ -557,10 +557,11 @@ __global__ __launch_bounds__(kTopThreads) void logits_topk_any_kernel(TeacherArg
 template <int DT, int PER>
 static hipError_t run_groups(const TeacherArgs &g, uint32_t shift, uint32_t n_groups, hipStream_t stream) {
   const uint32_t cap = g.a.k <= 512 ? 1024 : 2 * (uint32_t)ru4(g.a.k);
-  // (the bits that later take the place of the groups' keys and sums: at most a word for each vector, a load of four
-  // vectors a thread at most is half a group or more, so 8 bytes a group are enough)
-  const uint32_t dyn = 8 * n_groups + 8 * cap + 2 * n_groups;
-  logits_topk_groups_kernel<DT, PER><<<(uint32_t)g.a.rows, kTopThreads, dyn, stream>>>(g, shift, n_groups, cap);
+  // the groups' keys and sums, later a bit a logit (in whole words a thread)
+  const uint32_t bits = 32 * kTopThreads, words = (uint32_t)cdiv((uint64_t)row_vecs(g.a.vocab, DT, g.a.row_stride) * Num<DT>::E, bits) * kTopThreads;
+  const uint32_t region = 4 * (2 * n_groups > words ? 2 * n_groups : words);
+  const uint32_t dyn = region + 8 * cap + 2 * n_groups;
+  logits_topk_groups_kernel<DT, PER><<<(uint32_t)g.a.rows, kTopThreads, dyn, stream>>>(g, shift, n_groups, cap, region);
   return hipGetLastError();
 }
 
@@ -580,7 +581,7 @@ static hipError_t run_typed(const TeacherArgs &g, hipStream_t stream) {
   if (nv <= most) return run_groups<DT, 1>(g, 0, loads * 4 * T, stream);
   if (nv <= 2 * most) return run_groups<DT, 2>(g, 0, loads * 2 * T, stream);
   uint32_t shift = 0;
-  while ((loads >> shift) * T > most) ++shift;
+  while (cdiv(loads, 1u << shift) * T > most) ++shift;
   return run_groups<DT, 4>(g, shift, (uint32_t)cdiv(loads, 1u << shift) * T, stream);
 }
 

@@ -397,13 +397,15 @@ def test_offsets_past_32_bits(bpc):
     ws = workspace(bpc, d, 3)
     msg = torch.zeros(bpc.logits_message_bytes(d, 3), dtype=torch.uint8, device="cuda")
     bpc.bpc_logits_topk(d, view, None, msg, ws)
-    small = view.contiguous()
+    # (the order of a sum goes by where a row starts in its 128-byte line: 24 elements further each, here as there)
+    small = torch.empty(3, 1024 + 24, dtype=torch.bfloat16, device="cuda")[:, :vocab]
+    small.copy_(view)
     msg2 = torch.zeros_like(msg)
     bpc.bpc_logits_topk(d, small, None, msg2, ws)
     assert torch.equal(msg, msg2)
     m = make_messages(bpc, d, records)
     loss, loss2 = torch.zeros(3, device="cuda"), torch.zeros(3, device="cuda")
-    grad = torch.zeros_like(small)
+    grad = torch.zeros(3, vocab, dtype=torch.bfloat16, device="cuda")
     bpc.bpc_distill_step(d, small, m, None, None, loss2, grad, ws)
     bpc.bpc_distill_step(d, view, m, None, None, loss, view, ws)
     assert torch.equal(loss, loss2) and torch.equal(view, grad)
