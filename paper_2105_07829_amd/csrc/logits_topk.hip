@@ -7,6 +7,7 @@
 // formed as a difference.
 #include "distill.hpp"
 #include "kernels.hpp"
+#include <type_traits>
 
 namespace bpc {
 
@@ -188,14 +189,26 @@ struct Tally {
 
 constexpr int kTopThreads = 256;
 
+// Largest value and sum over 2, 4 or 8 neighbouring lanes, in all of them.
+template <int LANES, class Op>
+__device__ inline float lanes_all(float x, const Op &op) {
+  const auto from = [](float y, auto ctrl) {
+    return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(y), decltype(ctrl)::value, 0xf, 0xf, true));
+  };
+  if (LANES >= 2) x = op(x, from(x, std::integral_constant<int, 0xB1>{}));    // quad_perm: the other of a pair
+  if (LANES >= 4) x = op(x, from(x, std::integral_constant<int, 0x4E>{}));    // the other pair of a quad
+  if (LANES >= 8) x = op(x, from(x, std::integral_constant<int, 0x141>{}));   // row_half_mirror: the other quad
+  return x;
+}
+
 // Rows by groups.  One pass finds every group's largest logit and its sum of exponentials (relative to that logit); at
 // least k logits reach the k-th largest of the groups' largest (or a little less), so only the few groups that reach
-// it are looked through again for candidates.  A thread loads four vectors at a time, kTopThreads apart; PER of them
-// (1, 2, or 4 in each of 1 << shift such loads) make a group.
-template <int DT, int PER>
-__global__ __launch_bounds__(kTopThreads) void logits_topk_groups_kernel(TeacherArgs g, uint32_t shift, uint32_t n_groups, uint32_t cap,
-                                                                          uint32_t region) {
-  constexpr int E = Num<DT>::E, T = kTopThreads, Q = 4 / PER;
+// it are looked through again for candidates.  A group is LANES neighbouring vectors, up to a line of 128 bytes, so
+// that looking through it again moves no more than it holds (with groups of vectors 4 KB apart, 8192 x 131072 bf16,
+// k = 256, that moved a whole row again: 560 us).
+template <int DT, int LANES>
+__global__ __launch_bounds__(kTopThreads) void logits_topk_groups_kernel(TeacherArgs g, uint32_t n_groups, uint32_t cap, uint32_t region) {
+  constexpr int E = Num<DT>::E, T = kTopThreads;
   extern __shared__ __align__(16) uint8_t dyn[];
   __shared__ float lds[T / 64], lds_min[T / 64];
   __shared__ uint32_t counters[3], scan_lds[T / 64], before[T];
@@ -214,50 +227,51 @@ __global__ __launch_bounds__(kTopThreads) void logits_topk_groups_kernel(Teacher
   uint32_t *cidx = ckey + cap;
   uint16_t *glist = reinterpret_cast<uint16_t *>(cidx + cap);
   const Stretch all(row, 0, row.nv);
-  const uint32_t b0 = all.b0, b1 = all.b1, loads = (b1 - b0 + 4 * T - 1) / (4 * T);
+  const uint32_t b0 = all.b0, b1 = all.b1;
   const float c2 = g.c2;
   float top = kNegInf;
-  uint32_t done = 0;   // groups written
-  float m = kNegInf, s = 0.0f;
-  for (uint32_t b = 0; b < loads; ++b) {
+  const auto larger = [](float x, float y) { return fmaxf(x, y); };
+  const auto plus = [](float x, float y) { return x + y; };
+  for (uint32_t v = 0; v < n_groups * LANES; v += 4 * T) {
     u32x4 w[4];
-    const uint32_t v0 = b0 + b * 4 * T;
-    if (v0 + 4 * T <= b1) {
+    if (b0 + v + 4 * T <= b1) {
 #pragma unroll
-      for (int u = 0; u < 4; ++u) w[u] = row.load(v0 + u * T, threadIdx.x);
+      for (int u = 0; u < 4; ++u) w[u] = row.load_once(b0 + v + u * T, threadIdx.x);
     } else {
 #pragma unroll
-      for (int u = 0; u < 4; ++u) w[u] = v0 + u * T + threadIdx.x < b1 ? row.load(v0 + u * T, threadIdx.x) : Num<DT>::masked();
+      for (int u = 0; u < 4; ++u) {
+        w[u] = Num<DT>::masked();
+        if (b0 + v + u * T + threadIdx.x < b1) w[u] = row.load_once(b0 + v + u * T, threadIdx.x);
+      }
     }
+    float m[4], s[4];
 #pragma unroll
-    for (int q = 0; q < Q; ++q) {
-      float x[PER * E];
+    for (int u = 0; u < 4; ++u) {
+      float x[E];
+      Num<DT>::widen(w[u], x);
+      m[u] = x[0];
 #pragma unroll
-      for (int u = 0; u < PER; ++u) Num<DT>::widen(w[q * PER + u], x + u * E);
-      float nm = PER == 4 ? m : kNegInf;
+      for (int i = 1; i < E; ++i) m[u] = fmaxf(m[u], x[i]);
+      m[u] = lanes_all<LANES>(m[u], larger);
+      const float ref2 = base2_ref(m[u], c2);
+      s[u] = 0.0f;
 #pragma unroll
-      for (int i = 0; i < PER * E; ++i) nm = fmaxf(nm, x[i]);
-      const float ref2 = base2_ref(nm, c2);
-      float ns = PER == 4 ? s * exp2_hw(base2_ref(m, c2) - ref2) : 0.0f;
+      for (int i = 0; i < E; ++i) s[u] += base2_exp(x[i], c2, ref2);
+      s[u] = lanes_all<LANES>(s[u], plus);
+      top = fmaxf(top, m[u]);
+    }
+    if (threadIdx.x % LANES == 0) {
 #pragma unroll
-      for (int i = 0; i < PER * E; ++i) ns += base2_exp(x[i], c2, ref2);
-      m = nm;
-      s = ns;
-      if (PER != 4 || ((b + 1) & ((1u << shift) - 1)) == 0 || b + 1 == loads) {
-        gkey[done + threadIdx.x] = order_key(m);
-        gsum[done + threadIdx.x] = s;
-        top = fmaxf(top, m);
-        done += T;
-        m = kNegInf;
-        s = 0.0f;
+      for (int u = 0; u < 4; ++u) {
+        const uint32_t id = (v + u * T + threadIdx.x) / LANES;
+        gkey[id] = __float_as_uint(m[u]);
+        gsum[id] = s[u];
       }
     }
   }
-  for (; done < n_groups; done += T) {
-    gkey[done + threadIdx.x] = 0;
-    gsum[done + threadIdx.x] = 0.0f;
-  }
-  // every thread's largest logit is the largest of some groups: T of them reach the smallest of those
+  __syncthreads();
+  for (uint32_t i = threadIdx.x; i < n_groups; i += T) gkey[i] = order_key(__uint_as_float(gkey[i]));
+  // every LANES threads' largest logit is the largest of some group: T / LANES groups reach the smallest of those
   float least = -wave_max(-top);
   // the vectors beside the body are nobody's group: they are looked through in any case
   float edge[E];
@@ -295,7 +309,7 @@ __global__ __launch_bounds__(kTopThreads) void logits_topk_groups_kernel(Teacher
       }
       return tally.add(c);
     };
-    const uint32_t from = g.a.k <= T && least > kNegInf ? order_key(least) : kLowestKey;
+    const uint32_t from = g.a.k <= T / LANES && least > kNegInf ? order_key(least) : kLowestKey;
     low = kth_key(count, g.a.k, from, order_key(top), g.a.k / 8 + 4, &reach);
     if (low == 0) low = kLowestKey;
   }
@@ -337,11 +351,9 @@ __global__ __launch_bounds__(kTopThreads) void logits_topk_groups_kernel(Teacher
       }
     }
   };
-  const uint32_t vg_shift = (PER == 1 ? 0 : PER == 2 ? 1 : 2) + shift;
-  const uint32_t pairs = n_listed << vg_shift;
+  const uint32_t pairs = n_listed * LANES;
   for (uint32_t p = threadIdx.x; p < pairs; p += T) {
-    const uint32_t id = glist[p >> vg_shift], u = p & ((1u << vg_shift) - 1);
-    const uint32_t v = b0 + (((id / T) << vg_shift) + u) * T + id % T;
+    const uint32_t v = b0 + glist[p / LANES] * LANES + p % LANES;
     if (v < b1) {
       float x[E];
       Num<DT>::widen(row.load(0, v), x);
@@ -554,35 +566,35 @@ __global__ __launch_bounds__(kTopThreads) void logits_topk_any_kernel(TeacherArg
   select_any<DT, kTopThreads>(g, row, rec);
 }
 
-template <int DT, int PER>
-static hipError_t run_groups(const TeacherArgs &g, uint32_t shift, uint32_t n_groups, hipStream_t stream) {
-  const uint32_t cap = g.a.k <= 512 ? 1024 : 2 * (uint32_t)ru4(g.a.k);
+template <int DT, int LANES>
+static hipError_t run_groups(const TeacherArgs &g, uint32_t nv, hipStream_t stream) {
+  const uint32_t T = kTopThreads, n_groups = (uint32_t)cdiv(nv, 4 * T) * 4 * T / LANES;   // (of whole loads)
+  const uint32_t cap = 2 * (uint32_t)ru4(g.a.k) + 256;
   // the groups' keys and sums, later a bit a logit (in whole words a thread)
-  const uint32_t bits = 32 * kTopThreads, words = (uint32_t)cdiv((uint64_t)row_vecs(g.a.vocab, DT, g.a.row_stride) * Num<DT>::E, bits) * kTopThreads;
+  const uint32_t words = (uint32_t)cdiv((uint64_t)nv * Num<DT>::E, 32 * T) * T;
   const uint32_t region = 4 * (2 * n_groups > words ? 2 * n_groups : words);
   const uint32_t dyn = region + 8 * cap + 2 * n_groups;
-  logits_topk_groups_kernel<DT, PER><<<(uint32_t)g.a.rows, kTopThreads, dyn, stream>>>(g, shift, n_groups, cap, region);
+  logits_topk_groups_kernel<DT, LANES><<<(uint32_t)g.a.rows, kTopThreads, dyn, stream>>>(g, n_groups, cap, region);
   return hipGetLastError();
 }
 
 template <int DT>
 static hipError_t run_typed(const TeacherArgs &g, hipStream_t stream) {
-  const uint32_t nv = row_vecs(g.a.vocab, DT, g.a.row_stride), T = kTopThreads;
+  const uint32_t nv = row_vecs(g.a.vocab, DT, g.a.row_stride), k = g.a.k;
   if (nv > kChunkVecs) {
     logits_topk_any_kernel<DT><<<(uint32_t)g.a.rows, kTopThreads, 0, stream>>>(g);
     return hipGetLastError();
   }
-  if (nv < 2 * g.a.k && g.a.vocab <= kDenseVocab) {
+  if (nv < 2 * k && g.a.vocab <= kDenseVocab) {
     logits_topk_dense_kernel<DT><<<(uint32_t)g.a.rows, kTopThreads, 4 * g.a.vocab, stream>>>(g);
     return hipGetLastError();
   }
-  // (whole loads of four vectors, so that the groups of all threads are written)
-  const uint32_t most = g.a.k <= 512 ? 2048 : 4096, loads = (uint32_t)cdiv(nv, 4 * T);
-  if (nv <= most) return run_groups<DT, 1>(g, 0, loads * 4 * T, stream);
-  if (nv <= 2 * most) return run_groups<DT, 2>(g, 0, loads * 2 * T, stream);
-  uint32_t shift = 0;
-  while (cdiv(loads, 1u << shift) * T > most) ++shift;
-  return run_groups<DT, 4>(g, shift, (uint32_t)cdiv(loads, 1u << shift) * T, stream);
+  // The largest groups of which there are still two or more for each entry (then some 1.4 candidates an entry pass);
+  // never more than 4096.
+  if (nv >= 16 * k) return run_groups<DT, 8>(g, nv, stream);
+  if (nv >= 8 * k) return run_groups<DT, 4>(g, nv, stream);
+  if (nv >= 4 * k) return run_groups<DT, 2>(g, nv, stream);
+  return run_groups<DT, 1>(g, nv, stream);
 }
 
 hipError_t logits_topk(const DistillCall &call, uint8_t *out, uint8_t *ws, hipStream_t stream) {
