@@ -137,9 +137,17 @@ __device__ void select_any(const TeacherArgs &g, const Row<DT> &row, uint8_t *re
 
 // ---- rows whose k-th largest logit can be bounded from below by largest logits of groups
 
-__device__ inline float key_value(uint32_t key) {   // of a key that is neither 0 nor a NaN's
-  return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key);
-}
+// Keys without the low bits that logits of a type leave 0 as f32 (13 of f16, 16 of bf16): fewer steps for a bisection.
+template <int DT>
+struct Key {
+  static constexpr int S = DT == BPC_F32 ? 0 : DT == BPC_F16 ? 13 : 16;
+  static constexpr uint32_t kLowest = kLowestKey >> S;
+  static __device__ uint32_t of(float x) { return order_key(x) >> S; }
+  static __device__ float value(uint32_t key) {   // of a key that is neither 0 nor a NaN's
+    const uint32_t k = key << S | ((1u << S) - 1);
+    return __uint_as_float(k & 0x80000000u ? key << S & 0x7fffffffu : ~k);
+  }
+};
 
 // How many of a wave's keys reach `least`: a comparison each, the counting is the scalar unit's.
 __device__ inline uint32_t wave_count(uint32_t key, uint32_t least) { return (uint32_t)__popcll(__ballot(key >= least)); }
@@ -208,11 +216,12 @@ __device__ inline float lanes_all(float x, const Op &op) {
 // k = 256, that moved a whole row again: 560 us).
 template <int DT, int LANES>
 __global__ __launch_bounds__(kTopThreads) void logits_topk_groups_kernel(TeacherArgs g, uint32_t n_groups, uint32_t cap, uint32_t region) {
+  using K = Key<DT>;
   constexpr int E = Num<DT>::E, T = kTopThreads;
   extern __shared__ __align__(16) uint8_t dyn[];
-  __shared__ float lds[T / 64], lds_min[T / 64];
+  __shared__ float lds[T / 64];
   __shared__ uint32_t counters[3], scan_lds[T / 64], before[T];
-  __shared__ uint32_t n_cand, pick[2];
+  __shared__ uint32_t n_cand, n_level, pick[2];
   __shared__ unsigned long long left_sum;
   const uint64_t r = blockIdx.x;
   uint8_t *rec = g.out + uniform_off(r * g.a.message_stride);
@@ -270,9 +279,7 @@ __global__ __launch_bounds__(kTopThreads) void logits_topk_groups_kernel(Teacher
     }
   }
   __syncthreads();
-  for (uint32_t i = threadIdx.x; i < n_groups; i += T) gkey[i] = order_key(__uint_as_float(gkey[i]));
-  // every LANES threads' largest logit is the largest of some group: T / LANES groups reach the smallest of those
-  float least = -wave_max(-top);
+  for (uint32_t i = threadIdx.x; i < n_groups; i += T) gkey[i] = K::of(__uint_as_float(gkey[i]));
   // the vectors beside the body are nobody's group: they are looked through in any case
   float edge[E];
   uint32_t edge_v;
@@ -286,15 +293,12 @@ __global__ __launch_bounds__(kTopThreads) void logits_topk_groups_kernel(Teacher
       odd = odd || edge[i] != edge[i];
     }
   }
-  if ((threadIdx.x & 63) == 0) lds_min[threadIdx.x >> 6] = least;
   if (threadIdx.x == 0) {
     n_cand = 0;
+    n_level = 0;
     left_sum = 0;
   }
   top = all_max<T>(top, lds);
-  least = lds_min[0];
-#pragma unroll
-  for (int i = 1; i < T / 64; ++i) least = fminf(least, lds_min[i]);
   const float top2 = base2_ref(top, c2);
   uint32_t low = 0, reach;
   {
@@ -309,9 +313,19 @@ __global__ __launch_bounds__(kTopThreads) void logits_topk_groups_kernel(Teacher
       }
       return tally.add(c);
     };
-    const uint32_t from = g.a.k <= T / LANES && least > kNegInf ? order_key(least) : kLowestKey;
-    low = kth_key(count, g.a.k, from, order_key(top), g.a.k / 8 + 4, &reach);
-    if (low == 0) low = kLowestKey;
+    // (in steps down from the top first: a few are enough for logits of ordinary spread)
+    uint32_t from = K::kLowest, high = K::of(top);
+    for (float x = 2.0f; x < 1e5f; x *= 2.0f) {
+      const uint32_t key = K::of(top - x);
+      if (key <= K::kLowest) break;
+      if (count(key) >= g.a.k) {
+        from = key;
+        break;
+      }
+      high = key - 1;
+    }
+    low = kth_key(count, g.a.k, from, high, g.a.k / 8 + 4, &reach);
+    if (low == 0) low = K::kLowest;
   }
   float rest = 0.0f;   // relative to 2^top2
   uint32_t mine = 0, n_listed;
@@ -320,7 +334,7 @@ __global__ __launch_bounds__(kTopThreads) void logits_topk_groups_kernel(Teacher
     const float sum = gsum[i];
     odd = odd || sum != sum;
     if (key >= low) ++mine;
-    else if (key != 0) rest += sum * exp2_hw(base2_ref(key_value(key), c2) - top2);
+    else if (key != 0) rest += sum * exp2_hw(base2_ref(K::value(key), c2) - top2);
   }
   // (listed by a prefix sum, so that the sum over what these groups hold beside the candidates is always formed in
   // the same order)
@@ -331,7 +345,7 @@ __global__ __launch_bounds__(kTopThreads) void logits_topk_groups_kernel(Teacher
     select_any<DT, T>(g, row, rec);
     return;
   }
-  const float low_value = key_value(low);
+  const float low_value = K::value(low);
   const auto look = [&](const float *x, uint32_t j0) {
     float most = x[0];
 #pragma unroll
@@ -344,7 +358,7 @@ __global__ __launch_bounds__(kTopThreads) void logits_topk_groups_kernel(Teacher
         if (x[i] >= low_value) {
           const uint32_t to = atomicAdd(&n_cand, 1u);
           if (to < cap) {
-            ckey[to] = order_key(x[i]);
+            ckey[to] = K::of(x[i]);
             cidx[to] = j0 + i;
           }
         }
@@ -373,15 +387,7 @@ __global__ __launch_bounds__(kTopThreads) void logits_topk_groups_kernel(Teacher
   uint32_t kth = low, last = 0xffffffffu;
   if (take < cand) {
     constexpr uint32_t kOneWave = 512;
-    const uint32_t high = order_key(top);
-    const auto search = [&](const auto &count_keys, const auto &count_level) {
-      kth = kth_key(count_keys, take, low, high, 0, &reach);
-      if (reach > take) {
-        // too many are level with the k-th: out go those with the highest indices
-        const uint32_t above = kth == 0xffffffffu ? 0u : count_keys(kth + 1);
-        last = ~kth_key(count_level, take - above, 1u, 0xffffffffu, 0, &reach);
-      }
-    };
+    const uint32_t high = K::of(top);
     if (cand <= kOneWave) {   // (uniform) by one wave, out of its registers
       if (threadIdx.x < 64) {
         uint32_t key[kOneWave / 64];
@@ -390,66 +396,75 @@ __global__ __launch_bounds__(kTopThreads) void logits_topk_groups_kernel(Teacher
           const uint32_t e = threadIdx.x + i * 64;
           key[i] = e < cand ? ckey[e] : 0u;
         }
-        const auto count_keys = [&](uint32_t least_key) {
+        const auto count = [&](uint32_t least) {
           uint32_t c = 0;
 #pragma unroll
-          for (uint32_t i = 0; i < kOneWave / 64; ++i) c += wave_count(key[i], least_key);
+          for (uint32_t i = 0; i < kOneWave / 64; ++i)
+            if (i * 64 < cand) c += wave_count(key[i], least);
           return c;
         };
-        const auto count_level = [&](uint32_t least_key) {
-          uint32_t c = 0;
-          for (uint32_t i = 0; i < kOneWave / 64; ++i) {
-            const uint32_t e = threadIdx.x + i * 64;
-            c += wave_count(e < cand && ckey[e] == kth ? ~cidx[e] : 0u, least_key);
-          }
-          return c;
-        };
-        search(count_keys, count_level);
+        const uint32_t found = kth_key(count, take, low, high, 0, &reach);
+        const uint32_t above = reach > take ? count(found + 1) : 0;
         if (threadIdx.x == 0) {
-          pick[0] = kth;
-          pick[1] = last;
+          pick[0] = found;
+          pick[1] = reach > take ? take - above : 0xffffffffu;
         }
       }
-      __syncthreads();
-      kth = pick[0];
-      last = pick[1];
     } else {
       Tally tally(counters);
       const uint32_t rounds = (cand + T - 1) / T;
-      const auto count_keys = [&](uint32_t least_key) {
+      const auto count = [&](uint32_t least) {
         uint32_t c = 0;
         for (uint32_t i = 0; i < rounds; ++i) {
           const uint32_t e = threadIdx.x + i * T;
-          c += wave_count(e < cand ? ckey[e] : 0u, least_key);
+          c += wave_count(e < cand ? ckey[e] : 0u, least);
         }
         return tally.add(c);
       };
-      const auto count_level = [&](uint32_t least_key) {
-        uint32_t c = 0;
-        for (uint32_t i = 0; i < rounds; ++i) {
-          const uint32_t e = threadIdx.x + i * T;
-          c += wave_count(e < cand && ckey[e] == kth ? ~cidx[e] : 0u, least_key);
-        }
-        return tally.add(c);
-      };
-      search(count_keys, count_level);
+      const uint32_t found = kth_key(count, take, low, high, 0, &reach);
+      const uint32_t above = reach > take ? count(found + 1) : 0;
+      if (threadIdx.x == 0) {
+        pick[0] = found;
+        pick[1] = reach > take ? take - above : 0xffffffffu;
+      }
+    }
+    __syncthreads();
+    kth = pick[0];
+    const uint32_t open = pick[1];   // how many of those level with the k-th are listed (all of them: 2^32 - 1)
+    if (open != 0xffffffffu) {
+      // those with the lowest indices: their indices side by side, the one with open - 1 smaller ones is the last
+      uint32_t *level = gkey;
+      for (uint32_t i = threadIdx.x; i < cand; i += T)
+        if (ckey[i] == kth) level[atomicAdd(&n_level, 1u)] = cidx[i];
+      __syncthreads();
+      const uint32_t n = n_level;
+      for (uint32_t i = threadIdx.x; i < n; i += T) {
+        uint32_t smaller = 0;
+        for (uint32_t o = 0; o < n; ++o) smaller += level[o] < level[i] ? 1u : 0u;
+        if (smaller == open - 1) pick[1] = level[i];
+      }
+      __syncthreads();
+      last = pick[1];
     }
   }
   // index order: a bit a logit for what is listed (in place of the groups), a prefix sum over stretches of words
   uint32_t *bits = gkey;
-  const uint32_t span = (row.nv * E + 32 * T - 1) / (32 * T);   // words of a thread's stretch
-  for (uint32_t i = threadIdx.x; i < span * T; i += T) bits[i] = 0;
+  const uint32_t span = (row.nv * E + 128 * T - 1) / (128 * T) * 4;   // words of a thread's stretch, whole quads
+  for (uint32_t i = threadIdx.x; i < span / 4 * T; i += T) reinterpret_cast<uint4 *>(bits)[i] = uint4{0, 0, 0, 0};
   __syncthreads();
   const auto listed = [&](uint32_t i) { return ckey[i] > kth || (ckey[i] == kth && cidx[i] <= last); };
   float over = kNegInf;   // the largest candidate that is not listed
   for (uint32_t i = threadIdx.x; i < cand; i += T) {
     if (listed(i)) atomicOr(&bits[cidx[i] >> 5], 1u << (cidx[i] & 31));
-    else over = fmaxf(over, key_value(ckey[i]));
+    else over = fmaxf(over, K::value(ckey[i]));
   }
   __syncthreads();
   {
     uint32_t n = 0, all;
-    for (uint32_t i = 0; i < span; ++i) n += __popc(bits[threadIdx.x * span + i]);
+    for (uint32_t i = 0; i < span / 4; ++i) {
+      const uint4 q = reinterpret_cast<const uint4 *>(bits)[threadIdx.x * (span / 4) + i];
+      n += __popc(q.x) + __popc(q.y) + __popc(q.z) + __popc(q.w);
+    }
     before[threadIdx.x] = block_exclusive_scan<T>(n, scan_lds, &all);
   }
   if (take < cand) {
@@ -457,7 +472,7 @@ __global__ __launch_bounds__(kTopThreads) void logits_topk_groups_kernel(Teacher
     over = base2_ref(all_max<T>(over, lds), c2);
     unsigned long long sum = 0;
     for (uint32_t i = threadIdx.x; i < cand; i += T)
-      if (!listed(i)) sum += (unsigned long long)(base2_exp(key_value(ckey[i]), c2, over) * 0x1p40f);
+      if (!listed(i)) sum += (unsigned long long)(base2_exp(K::value(ckey[i]), c2, over) * 0x1p40f);
     if (sum) atomicAdd(&left_sum, sum);
   }
   __syncthreads();
@@ -467,7 +482,7 @@ __global__ __launch_bounds__(kTopThreads) void logits_topk_groups_kernel(Teacher
     uint32_t place = before[stretch];
     for (uint32_t q = stretch * span; q < word; ++q) place += __popc(bits[q]);
     place += __popc(bits[word] & ((1u << (j & 31)) - 1));
-    if (place < g.a.k) put_entry(g, rec, place, j, key_value(ckey[i]) - top);
+    if (place < g.a.k) put_entry(g, rec, place, j, K::value(ckey[i]) - top);
   }
   rest = all_sum<T>(rest, lds);
   if (take < cand) rest += (float)left_sum * 0x1p-40f * exp2_hw(over - top2);
@@ -570,9 +585,11 @@ template <int DT, int LANES>
 static hipError_t run_groups(const TeacherArgs &g, uint32_t nv, hipStream_t stream) {
   const uint32_t T = kTopThreads, n_groups = (uint32_t)cdiv(nv, 4 * T) * 4 * T / LANES;   // (of whole loads)
   const uint32_t cap = 2 * (uint32_t)ru4(g.a.k) + 256;
-  // the groups' keys and sums, later a bit a logit (in whole words a thread)
-  const uint32_t words = (uint32_t)cdiv((uint64_t)nv * Num<DT>::E, 32 * T) * T;
-  const uint32_t region = 4 * (2 * n_groups > words ? 2 * n_groups : words);
+  // the groups' keys and sums, later the indices level with the k-th, then a bit a
+  // logit (in whole quads of words a thread)
+  const uint32_t words = (uint32_t)cdiv((uint64_t)nv * Num<DT>::E, 128 * T) * 4 * T;
+  uint32_t region = 8 * n_groups > 4 * words ? 8 * n_groups : 4 * words;
+  if (region < 4 * cap) region = 4 * cap;
   const uint32_t dyn = region + 8 * cap + 2 * n_groups;
   logits_topk_groups_kernel<DT, LANES><<<(uint32_t)g.a.rows, kTopThreads, dyn, stream>>>(g, n_groups, cap, region);
   return hipGetLastError();
