@@ -351,100 +351,107 @@ def distill_workspace_bytes(d: Distill, rows: int) -> int:
     return int(lib().bpc_distill_workspace_bytes(C.byref(d), rows))
 
 
-_LOGITS_DTYPES = {"torch.float32": F32, "torch.float16": F16, "torch.bfloat16": BF16}
-_logits_codes = {}
+_logits_codes = {}   # torch dtype -> code, filled at the first call
+_types = None        # torch.uint8, torch.float32, torch.int64
 
 
-def _logits(t, d, what):
-    """(dtype code, rows, row stride) of a GPU tensor [rows, vocab] whose rows are contiguous; the stride
-    of a single row is its length, whatever the tensor says."""
-    code = _logits_codes.get(t.dtype)
-    if code is None:
-        code = _LOGITS_DTYPES.get(str(t.dtype))
-        if code is None:
-            raise TypeError(f"{what} dtype {t.dtype} not supported")
-        _logits_codes[t.dtype] = code
-    if t.dim() != 2 or t.shape[1] != d.vocab or (d.vocab > 1 and t.stride(1) != 1):
-        raise ValueError(f"{what}: expected [rows, {d.vocab}] with contiguous rows, got {tuple(t.shape)}, strides {t.stride()}")
-    rows = t.shape[0]
-    return code, rows, (t.stride(0) if rows > 1 else d.vocab)
-
-
-def _per_row(t, dtype, rows, what, per=1, optional=True):
-    """A contiguous tensor of at least ``per`` elements a row; its pointer."""
-    if t is None:
-        if optional:
-            return None
-        raise ValueError(f"{what} missing")
-    if str(t.dtype) != dtype or t.numel() < rows * per or not t.is_contiguous():
-        raise ValueError(f"{what}: expected a contiguous {dtype} tensor of at least {rows * per} elements, got {tuple(t.shape)} {t.dtype}")
-    return t.data_ptr()
-
-
-def _same_device(*tensors):
-    """The kernels run on the current device: every tensor has to be there."""
-    global _torch
-    if _torch is None:
+def _distill_torch():
+    """The torch types that the calls below compare with, and the current device (an int; -1 without a GPU).  Kept
+    to plain attributes and integers: a call spends about as long here as in the launch."""
+    global _torch, _types
+    if _types is None:
         import torch
 
         _torch = torch
-    at = _torch.cuda.current_device() if _torch.cuda.is_available() else -1
-    for t in tensors:
-        if t is not None and (not t.is_cuda or t.get_device() != at):
-            raise ValueError(f"tensor on {t.device}, the current device is cuda:{at}")
+        _logits_codes.update({torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16})
+        _types = torch.uint8, torch.float32, torch.int64
+    if _torch.cuda.is_initialized():
+        return _torch._C._cuda_getDevice()
+    return _torch.cuda.current_device() if _torch.cuda.is_available() else -1
+
+
+def _logits(t, d, at, what="logits"):
+    """(pointer, dtype code, row stride, rows) of a tensor [rows, vocab] on the current device whose rows are
+    contiguous; the stride of a single row is its length, whatever the tensor says."""
+    code, shape = _logits_codes.get(t.dtype), t.shape
+    if code is None:
+        raise TypeError(f"{what} dtype {t.dtype} not supported")
+    if len(shape) != 2 or shape[1] != d.vocab or (t.stride(1) != 1 and d.vocab > 1):
+        raise ValueError(f"{what}: expected [rows, {d.vocab}] with contiguous rows, got {tuple(shape)}, strides {t.stride()}")
+    if t.get_device() != at or at < 0:
+        raise ValueError(f"{what} on {t.device}, the current device is cuda:{at}")
+    rows = shape[0]
+    return t.data_ptr(), code, (t.stride(0) if rows > 1 else shape[1]), rows
+
+
+def _flat(t, dtype, n, at, what):
+    """Pointer of a contiguous tensor of at least ``n`` elements on the current device."""
+    if t.dtype is not dtype or t.numel() < n or not t.is_contiguous():
+        raise ValueError(f"{what}: expected a contiguous {dtype} tensor of at least {n} elements, got {tuple(t.shape)} {t.dtype}")
+    if t.get_device() != at or at < 0:
+        raise ValueError(f"{what} on {t.device}, the current device is cuda:{at}")
+    return t.data_ptr()
+
+
+def _record_bytes(d):
+    """bpc_logits_stride of a valid description."""
+    k = d.k
+    return 16 + (k + 3 & ~3) * 4 + ((k + 3 & ~3) if d.kind == TOPK else ((k + 1) // 2 + 3 & ~3)) * 4
 
 
 def bpc_logits_topk(d: Distill, logits, row_weight, messages, ws, stream=None) -> None:
     """messages = the k largest logits of every row of ``logits`` [rows, vocab] and the mass of the rest."""
-    code, rows, stride = _logits(logits, d, "logits")
-    _same_device(logits, row_weight, messages, ws)
-    st = lib().bpc_logits_topk(C.byref(d), logits.data_ptr(), code, stride, rows,
-                               _per_row(row_weight, "torch.float32", rows, "row_weight"),
-                               _per_row(messages, "torch.uint8", rows, "messages", logits_stride(d), False),
-                               _ptr(ws), ws.numel() * ws.element_size(), _stream(stream))
+    at = _distill_torch()
+    u8, f32, _ = _types
+    ptr, code, stride, rows = _logits(logits, d, at)
+    st = lib().bpc_logits_topk(C.byref(d), ptr, code, stride, rows,
+                               None if row_weight is None else _flat(row_weight, f32, rows, at, "row_weight"),
+                               _flat(messages, u8, rows * _record_bytes(d), at, "messages"),
+                               _flat(ws, u8, 0, at, "ws"), ws.numel(), _stream(stream))
     _check(st, "bpc_logits_topk")
 
 
-def _student(d, logits, messages, labels, row_weight):
-    code, rows, stride = _logits(logits, d, "logits")
-    return rows, (C.byref(d), logits.data_ptr(), code, stride, rows,
-                  _per_row(messages, "torch.uint8", rows, "messages", logits_stride(d), False),
-                  _per_row(labels, "torch.int64", rows, "labels"),
-                  _per_row(row_weight, "torch.float32", rows, "row_weight"))
+def _student(d, logits, messages, labels, row_weight, at):
+    u8, f32, i64 = _types
+    ptr, code, stride, rows = _logits(logits, d, at)
+    return rows, (C.byref(d), ptr, code, stride, rows, _flat(messages, u8, rows * _record_bytes(d), at, "messages"),
+                  None if labels is None else _flat(labels, i64, rows, at, "labels"),
+                  None if row_weight is None else _flat(row_weight, f32, rows, at, "row_weight"))
 
 
-def _gradient(grad, logits, d, rows):
-    code, grows, stride = _logits(grad, d, "grad")
-    if grad.dtype != logits.dtype or grows != rows:
+def _gradient(grad, logits, d, rows, at):
+    ptr, _, stride, grows = _logits(grad, d, at, "grad")
+    if grad.dtype is not logits.dtype or grows != rows:
         raise ValueError(f"grad: expected {tuple(logits.shape)} {logits.dtype}, got {tuple(grad.shape)} {grad.dtype}")
-    return grad.data_ptr(), stride
+    return ptr, stride
 
 
 def bpc_distill_loss(d: Distill, logits, messages, labels, row_weight, loss, stats, ws, stream=None) -> None:
     """loss[r] of the student's ``logits`` [rows, vocab] against the teacher's messages (and ``labels``, or
     None); ``stats``: uint8 [rows, 32] for bpc_distill_grad, or None."""
-    rows, args = _student(d, logits, messages, labels, row_weight)
-    _same_device(logits, messages, labels, row_weight, loss, stats, ws)
-    st = lib().bpc_distill_loss(*args, _per_row(loss, "torch.float32", rows, "loss", 1, False),
-                                _per_row(stats, "torch.uint8", rows, "stats", DISTILL_STATS_BYTES),
-                                _ptr(ws), ws.numel() * ws.element_size(), _stream(stream))
+    at = _distill_torch()
+    u8, f32, _ = _types
+    rows, args = _student(d, logits, messages, labels, row_weight, at)
+    st = lib().bpc_distill_loss(*args, _flat(loss, f32, rows, at, "loss"),
+                                None if stats is None else _flat(stats, u8, rows * DISTILL_STATS_BYTES, at, "stats"),
+                                _flat(ws, u8, 0, at, "ws"), ws.numel(), _stream(stream))
     _check(st, "bpc_distill_loss")
 
 
 def bpc_distill_grad(d: Distill, logits, messages, labels, row_weight, stats, grad, stream=None) -> None:
     """grad = d sum(loss) / d logits from the statistics of bpc_distill_loss; ``grad`` may be ``logits``."""
-    rows, args = _student(d, logits, messages, labels, row_weight)
-    _same_device(logits, messages, labels, row_weight, stats, grad)
-    st = lib().bpc_distill_grad(*args, _per_row(stats, "torch.uint8", rows, "stats", DISTILL_STATS_BYTES, False),
-                                *_gradient(grad, logits, d, rows), _stream(stream))
+    at = _distill_torch()
+    rows, args = _student(d, logits, messages, labels, row_weight, at)
+    st = lib().bpc_distill_grad(*args, _flat(stats, _types[0], rows * DISTILL_STATS_BYTES, at, "stats"),
+                                *_gradient(grad, logits, d, rows, at), _stream(stream))
     _check(st, "bpc_distill_grad")
 
 
 def bpc_distill_step(d: Distill, logits, messages, labels, row_weight, loss, grad, ws, stream=None) -> None:
     """bpc_distill_loss and bpc_distill_grad in one call."""
-    rows, args = _student(d, logits, messages, labels, row_weight)
-    _same_device(logits, messages, labels, row_weight, loss, grad, ws)
-    st = lib().bpc_distill_step(*args, _per_row(loss, "torch.float32", rows, "loss", 1, False),
-                                *_gradient(grad, logits, d, rows), _ptr(ws), ws.numel() * ws.element_size(),
-                                _stream(stream))
+    at = _distill_torch()
+    u8, f32, _ = _types
+    rows, args = _student(d, logits, messages, labels, row_weight, at)
+    st = lib().bpc_distill_step(*args, _flat(loss, f32, rows, at, "loss"), *_gradient(grad, logits, d, rows, at),
+                                _flat(ws, u8, 0, at, "ws"), ws.numel(), _stream(stream))
     _check(st, "bpc_distill_step")

@@ -214,10 +214,10 @@ __device__ inline float lanes_all(float x, const Op &op) {
 // it are looked through again for candidates.  A group is LANES neighbouring vectors, up to a line of 128 bytes, so
 // that looking through it again moves no more than it holds (with groups of vectors 4 KB apart, 8192 x 131072 bf16,
 // k = 256, that moved a whole row again: 560 us).
-template <int DT, int LANES>
-__global__ __launch_bounds__(kTopThreads) void logits_topk_groups_kernel(TeacherArgs g, uint32_t n_groups, uint32_t cap, uint32_t region) {
+template <int DT, int LANES, int T>
+__global__ __launch_bounds__(T) void logits_topk_groups_kernel(TeacherArgs g, uint32_t n_groups, uint32_t cap, uint32_t region) {
   using K = Key<DT>;
-  constexpr int E = Num<DT>::E, T = kTopThreads;
+  constexpr int E = Num<DT>::E;
   extern __shared__ __align__(16) uint8_t dyn[];
   __shared__ float lds[T / 64];
   __shared__ uint32_t counters[3], scan_lds[T / 64], before[T];
@@ -366,12 +366,22 @@ __global__ __launch_bounds__(kTopThreads) void logits_topk_groups_kernel(Teacher
     }
   };
   const uint32_t pairs = n_listed * LANES;
-  for (uint32_t p = threadIdx.x; p < pairs; p += T) {
-    const uint32_t v = b0 + glist[p / LANES] * LANES + p % LANES;
-    if (v < b1) {
-      float x[E];
-      Num<DT>::widen(row.load(0, v), x);
-      look(x, v * E - row.off);
+  for (uint32_t p0 = 0; p0 < pairs; p0 += 4 * T) {   // (four loads on their way at a time)
+    uint32_t v[4];
+    u32x4 w[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const uint32_t p = p0 + u * T + threadIdx.x;
+      v[u] = p < pairs ? b0 + glist[p / LANES] * LANES + p % LANES : b1;
+      if (v[u] < b1) w[u] = row.load(0, v[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (v[u] < b1) {
+        float x[E];
+        Num<DT>::widen(w[u], x);
+        look(x, v[u] * E - row.off);
+      }
     }
   }
   if (has_edge) look(edge, edge_v * E - row.off);
@@ -581,9 +591,9 @@ __global__ __launch_bounds__(kTopThreads) void logits_topk_any_kernel(TeacherArg
   select_any<DT, kTopThreads>(g, row, rec);
 }
 
-template <int DT, int LANES>
+template <int DT, int LANES, int T>
 static hipError_t run_groups(const TeacherArgs &g, uint32_t nv, hipStream_t stream) {
-  const uint32_t T = kTopThreads, n_groups = (uint32_t)cdiv(nv, 4 * T) * 4 * T / LANES;   // (of whole loads)
+  const uint32_t n_groups = (uint32_t)cdiv(nv, 4 * T) * 4 * T / LANES;   // (of whole loads)
   const uint32_t cap = 2 * (uint32_t)ru4(g.a.k) + 256;
   // the groups' keys and sums, later the indices level with the k-th, then a bit a
   // logit (in whole quads of words a thread)
@@ -591,8 +601,18 @@ static hipError_t run_groups(const TeacherArgs &g, uint32_t nv, hipStream_t stre
   uint32_t region = 8 * n_groups > 4 * words ? 8 * n_groups : 4 * words;
   if (region < 4 * cap) region = 4 * cap;
   const uint32_t dyn = region + 8 * cap + 2 * n_groups;
-  logits_topk_groups_kernel<DT, LANES><<<(uint32_t)g.a.rows, kTopThreads, dyn, stream>>>(g, n_groups, cap, region);
+  logits_topk_groups_kernel<DT, LANES, T><<<(uint32_t)g.a.rows, T, dyn, stream>>>(g, n_groups, cap, region);
   return hipGetLastError();
+}
+
+// The largest groups of which there are still two or more for each entry (then some 1.4 candidates an entry pass);
+// never more than 4096.
+template <int DT, int T>
+static hipError_t run_lanes(const TeacherArgs &g, uint32_t nv, hipStream_t stream) {
+  if (nv >= 16 * g.a.k) return run_groups<DT, 8, T>(g, nv, stream);
+  if (nv >= 8 * g.a.k) return run_groups<DT, 4, T>(g, nv, stream);
+  if (nv >= 4 * g.a.k) return run_groups<DT, 2, T>(g, nv, stream);
+  return run_groups<DT, 1, T>(g, nv, stream);
 }
 
 template <int DT>
@@ -606,12 +626,10 @@ static hipError_t run_typed(const TeacherArgs &g, hipStream_t stream) {
     logits_topk_dense_kernel<DT><<<(uint32_t)g.a.rows, kTopThreads, 4 * g.a.vocab, stream>>>(g);
     return hipGetLastError();
   }
-  // The largest groups of which there are still two or more for each entry (then some 1.4 candidates an entry pass);
-  // never more than 4096.
-  if (nv >= 16 * k) return run_groups<DT, 8>(g, nv, stream);
-  if (nv >= 8 * k) return run_groups<DT, 4>(g, nv, stream);
-  if (nv >= 4 * k) return run_groups<DT, 2>(g, nv, stream);
-  return run_groups<DT, 1>(g, nv, stream);
+  // Rows that fill the device take 256 threads (512: 98 -> 119 us for 4096 x 50257 bf16), fewer than that 1024 (one row
+  // of 50,257 f32 in 20 us with 256 threads), rows of a few loads one wave.
+  if (nv <= 512) return run_lanes<DT, 64>(g, nv, stream);
+  return g.a.rows >= 512 ? run_lanes<DT, 256>(g, nv, stream) : run_lanes<DT, 1024>(g, nv, stream);
 }
 
 hipError_t logits_topk(const DistillCall &call, uint8_t *out, uint8_t *ws, hipStream_t stream) {

@@ -164,6 +164,17 @@ def test_topk_hard_rows(bpc, dtype, vocab):
 
 
 @pytest.mark.parametrize("dtype", DT)
+def test_topk_many_rows(bpc, dtype):
+    """Enough rows that a smaller workgroup takes each, hard ones among them."""
+    vocab = 9001
+    hard = np.stack([row for _, row in shapes_of_rows(vocab)])
+    x = np.random.default_rng(21).standard_normal((540, vocab)) * 2
+    x[7:7 + len(hard)] = hard
+    for k, kind in [(5, bpc.TOPK), (100, bpc.TOPK16), (900, bpc.TOPK)]:
+        check_topk(bpc, bpc.make_distill(kind, vocab, k, temperature=1.5), x, dtype, pad=3)
+
+
+@pytest.mark.parametrize("dtype", DT)
 def test_topk_lowest_of_the_type(bpc, dtype):
     import torch
     low = torch.finfo(tdtype(dtype)).min
@@ -296,6 +307,22 @@ def test_student_rows(bpc, dtype, rows):
     labels = list(rs.integers(-2, 1502, rows))
     weight = np.where(np.arange(rows) % 4 == 2, 0.0, rs.random(rows) - 0.3).astype(np.float32)
     check_student(bpc, describe(bpc, 1500, 40, tail=1, temperature=3.0, hard_weight=0.2), x, records, dtype, 1, 1, labels, weight)
+
+
+@pytest.mark.parametrize("dtype,hard,tau,tail", [("bf16", 0.2, 2.0, 1), ("f32", 0.0, 1.0, 0), ("f16", 0.1, 1.7, 1), ("f32", 0.3, 4.0, 1)])
+def test_student_many_rows(bpc, dtype, hard, tau, tail):
+    """Enough rows that a smaller workgroup takes each, odd ones among them."""
+    rs = np.random.default_rng(22)
+    vocab = 9001
+    x, records = make_case(rs, vocab, 300, 1030)
+    x[3] = np.nan
+    x[4, 17] = np.inf
+    x[5] *= 2e4 if dtype != "f16" else 1e3
+    x[6, 4000:] = {"f32": -3.4028234663852886e38, "f16": -65504.0, "bf16": -3.3895313892515355e38}[dtype]
+    x[6, 4000 + int(rs.integers(5000))] = 1.0
+    weight = np.where(np.arange(1030) % 9 == 8, 0.0, 1.0)
+    check_student(bpc, describe(bpc, vocab, 300, tail=tail, temperature=tau, hard_weight=hard), x, records, dtype, 1, 1,
+                  list(rs.integers(0, vocab, 1030)), weight, want_nan=(3, 4))
 
 
 @pytest.mark.parametrize("tail", [0, 1])

@@ -114,35 +114,38 @@ def test_workspace_grows_with_rows(bpc):
             assert all(s % 256 == 0 for s in sizes)
 
 
-def test_binding_refuses_what_the_kernels_cannot_take(bpc):
+def test_binding_refuses_what_the_kernels_cannot_take(bpc, monkeypatch):
+    """On CPU tensors that are taken for tensors of the current device: nothing is launched, the library is not called."""
     d = bpc.make_distill(bpc.TOPK, 100, 4)
     x = torch.zeros(3, 100)
     msg = torch.zeros(3 * bpc.logits_stride(d), dtype=torch.uint8)
     loss, stats, ws = torch.zeros(3), torch.zeros(3, 32, dtype=torch.uint8), torch.zeros(256, dtype=torch.uint8)
-    with pytest.raises(ValueError, match="current device"):     # everything on the CPU
-        bpc.bpc_logits_topk(d, x, None, msg, ws)
-    with pytest.raises(ValueError, match="current device"):
-        bpc.bpc_distill_step(d, x, msg, None, None, loss, x, ws)
+    for at in (-1, 0):                                          # no GPU, and everything on the CPU
+        monkeypatch.setattr(bpc, "_distill_torch", lambda at=at, real=bpc._distill_torch: (real(), at)[1])
+        with pytest.raises(ValueError, match="current device"):
+            bpc.bpc_logits_topk(d, x, None, msg, ws)
+        with pytest.raises(ValueError, match="current device"):
+            bpc.bpc_distill_step(d, x, msg, None, None, loss, x, ws)
     with pytest.raises(TypeError):
         bpc.bpc_distill_loss(d, x.double(), msg, None, None, loss, stats, ws)
-    with pytest.raises(ValueError):
-        bpc.bpc_distill_loss(d, x[:, :99], msg, None, None, loss, stats, ws)
-    with pytest.raises(ValueError):
-        bpc.bpc_distill_loss(d, torch.zeros(100, 3).t(), msg, None, None, loss, stats, ws)
-    with pytest.raises(ValueError):
-        bpc.bpc_distill_loss(d, x, msg[:-1], None, None, loss, stats, ws)
-    with pytest.raises(ValueError):
-        bpc.bpc_distill_loss(d, x, msg, torch.zeros(3, dtype=torch.int32), None, loss, stats, ws)
-    with pytest.raises(ValueError):
-        bpc.bpc_distill_loss(d, x, msg, None, torch.zeros(2), loss, stats, ws)
-    with pytest.raises(ValueError):
-        bpc.bpc_distill_loss(d, x, msg, None, None, None, stats, ws)
-    with pytest.raises(ValueError):
-        bpc.bpc_distill_grad(d, x, msg, None, None, None, x)
-    with pytest.raises(ValueError):
-        bpc.bpc_distill_grad(d, x, msg, None, None, stats, x.half())
-    with pytest.raises(ValueError):
-        bpc.bpc_distill_grad(d, x, msg, None, None, stats, torch.zeros(2, 100))
+    for bad in (x[:, :99], torch.zeros(100, 3).t(), x[0], x[None]):
+        with pytest.raises(ValueError, match="logits"):
+            bpc.bpc_distill_loss(d, bad, msg, None, None, loss, stats, ws)
+    u8, f32, i64 = bpc._types
+    for bad in (msg[:-1], msg.float(), torch.zeros(2, msg.numel(), dtype=u8)[:, ::2]):
+        with pytest.raises(ValueError, match="messages: expected"):
+            bpc._flat(bad, u8, 3 * bpc._record_bytes(d), -1, "messages")
+    for dtype, per in ((i64, 1), (f32, 1), (u8, 32)):
+        for bad in (torch.zeros(3 * per - 1, dtype=dtype), torch.zeros(3 * per, dtype=torch.int32), torch.zeros(3 * per, 2, dtype=dtype)[:, 0]):
+            with pytest.raises(ValueError, match="expected a contiguous"):
+                bpc._flat(bad, dtype, 3 * per, 0, "it")
+
+
+def test_binding_knows_the_record(bpc):
+    for kind in (bpc.TOPK, bpc.TOPK16):
+        for k in (1, 2, 3, 4, 5, 7, 8, 9, 100, 1023, 1024):
+            d = bpc.make_distill(kind, 5000, k)
+            assert bpc._record_bytes(d) == bpc.logits_stride(d)
 
 
 @pytest.mark.parametrize("tail_rest", [False, True])
