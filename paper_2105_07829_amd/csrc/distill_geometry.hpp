@@ -36,20 +36,32 @@ inline uint32_t row_vecs(uint32_t vocab, int dtype, uint64_t row_stride) {
   return (uint32_t)cdiv(vocab + (row_stride % e ? e - 1 : 0), e);
 }
 
+constexpr uint32_t kFewRows = 32, kLongVecs = 4096, kLeastVecs = 512, kFillChunks = 256;
 constexpr uint32_t kGradVecs = 16384;   // vectors of a row whose gradient one workgroup writes
 
-// Rows are cut into chunks, a workgroup each, where one workgroup may not have them whole.
+// How the sums over a row are formed: by one workgroup, or by one for each of its chunks and a launch that joins them.
+// One workgroup holds a bit a logit in LDS and, for loss and gradient in one call, the row in registers.
 struct Cut {
   uint32_t chunks;   // a row
-  uint32_t vecs;     // of a chunk
+  uint32_t vecs;     // of a chunk, at most kChunkVecs
 };
-inline Cut cut_rows(uint64_t rows, uint32_t vocab, int dtype, uint64_t row_stride) {
-  (void)rows;
-  Cut c;
-  c.chunks = (uint32_t)cdiv(row_vecs(vocab, dtype, row_stride), kChunkVecs);
-  c.vecs = (uint32_t)cdiv(row_vecs(vocab, dtype, row_stride), c.chunks);
-  return c;
+constexpr uint32_t kMarkWords = 1u << 18;   // logits that have a bit in LDS
+inline Cut cut_rows(uint64_t rows, uint32_t vocab, int dtype, uint64_t row_stride, bool step) {
+  const uint32_t nv = row_vecs(vocab, dtype, row_stride), e = 16 / elem_bytes(dtype);
+  const bool whole = step ? nv <= kChunkVecs : (uint64_t)nv * e <= kMarkWords;
+  // Few long rows of which only the loss is wanted are cut, too: 8 x 151,936 bf16 9.4 us cut and 16.1 whole, 1 x 50,257
+  // 9.0 and 10.4; 64 x 50,257 11.5 and 11.0.
+  if (whole && (step || rows > kFewRows || nv < kLongVecs)) return {1, nv};
+  uint64_t chunks = cdiv(kFillChunks, rows);   // for every compute unit
+  const uint64_t most = cdiv(nv, kLeastVecs), least = cdiv(nv, kChunkVecs);
+  chunks = chunks < most ? chunks : most;
+  chunks = chunks > least ? chunks : least;
+  return {(uint32_t)chunks, (uint32_t)cdiv(nv, chunks)};
 }
+
+// Rows of which the teacher's call keeps the largest logits and sums of groups: at most 4096 groups of at most 16
+// vectors, and a bit a logit in the 32 KB that these take.
+constexpr uint32_t kMostGroups = 4096, kGroupVecs = 16 * kMostGroups, kGroupWords = 64 * kMostGroups;
 
 constexpr uint32_t kPartialFloats = 4;   // what a chunk hands on: largest logit, sums at both temperatures
 constexpr uint32_t kStatsFloats = BPC_DISTILL_STATS_BYTES / 4;
@@ -70,16 +82,16 @@ inline DistillWs distill_ws(uint64_t rows, const Cut &cut) {
   return w;
 }
 
-// Of every call of `rows` rows (or fewer) whatever the type: what bpc_distill_workspace_bytes answers.
+// Enough for every call of `rows` rows or fewer, whatever the type and the stride: what bpc_distill_workspace_bytes
+// answers.  (cut_rows makes at most rows * (chunks that a row needs) chunks, or kFillChunks + rows.)
 inline size_t distill_workspace(const bpc_distill_t *d, uint64_t rows) {
-  size_t most = 256;
-  for (int dtype = BPC_F32; dtype <= BPC_BF16; ++dtype) {
-    for (uint64_t stride = 0; stride < 2; ++stride) {   // aligned rows and others
-      const size_t s = distill_ws(rows, cut_rows(rows, d->vocab, dtype, stride)).total;
-      if (s > most) most = s;
-    }
-  }
-  return most;
+  const uint64_t nv = row_vecs(d->vocab, BPC_F32, 1);   // (the type with most vectors, unaligned)
+  if (nv < kLongVecs && nv <= kChunkVecs) return 256;
+  const uint64_t whole = rows * cdiv(nv, kChunkVecs), fill = kFillChunks + rows;
+  const size_t partial = (size_t)(whole > fill ? whole : fill) * kPartialFloats * 4;
+  const size_t student = (partial + 255) / 256 * 256 + ((size_t)rows * BPC_DISTILL_STATS_BYTES + 255) / 256 * 256;
+  const size_t teacher = (size_t)(rows < kFewRows ? rows : kFewRows) * kMostGroups * 8;
+  return student > teacher ? student : teacher;
 }
 
 }  // namespace bpc

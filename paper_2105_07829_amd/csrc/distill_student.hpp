@@ -551,9 +551,9 @@ __device__ inline void put_stats(const Args &g, uint64_t r, const Stats &st) {
 }
 
 // Whole rows, a workgroup each: the loss.
-template <int DT, int HARD, int T, uint32_t MOST>
+template <int DT, int HARD, int T>
 __global__ __launch_bounds__(T) void distill_loss_kernel(Args g) {
-  __shared__ uint32_t bits[MOST * Num<DT>::E / 32];
+  extern __shared__ uint32_t bits[];   // (TAIL_REST)
   __shared__ FinishLds<T> lds;
   const uint64_t r = blockIdx.x;
   const float weight = weight_of(g, r);
@@ -792,11 +792,12 @@ static hipError_t held_rows(const Args &g, hipStream_t stream) {
 template <int DT, int HARD>
 static hipError_t run_typed(Args g, DistillRole role, uint8_t *ws, hipStream_t stream) {
   const uint32_t rows = (uint32_t)g.a.rows, nv = row_vecs(g.a.vocab, DT, g.a.row_stride);
-  const Cut cut = cut_rows(g.a.rows, g.a.vocab, DT, g.a.row_stride);
+  const Cut cut = cut_rows(g.a.rows, g.a.vocab, DT, g.a.row_stride, role == DistillRole::step);
   if (role == DistillRole::loss && cut.chunks == 1) {
-    if (nv <= 1024 && g.a.k <= kOneWaveK) distill_loss_kernel<DT, HARD, 64, 1024><<<rows, 64, 0, stream>>>(g);
-    else if (rows >= 1024) distill_loss_kernel<DT, HARD, 256, kChunkVecs><<<rows, 256, 0, stream>>>(g);
-    else distill_loss_kernel<DT, HARD, 1024, kChunkVecs><<<rows, 1024, 0, stream>>>(g);
+    const uint32_t dyn = g.a.rest_too ? (uint32_t)cdiv((uint64_t)nv * Num<DT>::E, 32) * 4 : 0;
+    if (nv <= 1024 && g.a.k <= kOneWaveK) distill_loss_kernel<DT, HARD, 64><<<rows, 64, dyn, stream>>>(g);
+    else if (rows >= 512) distill_loss_kernel<DT, HARD, 256><<<rows, 256, dyn, stream>>>(g);
+    else distill_loss_kernel<DT, HARD, 1024><<<rows, 1024, dyn, stream>>>(g);
     return hipGetLastError();
   }
   if (role == DistillRole::step && cut.chunks == 1) {

@@ -197,7 +197,7 @@ struct Tally {
 
 constexpr int kTopThreads = 256;
 
-// Largest value and sum over 2, 4 or 8 neighbouring lanes, in all of them.
+// Largest value and sum over 2, 4, 8 or 16 neighbouring lanes, in all of them.
 template <int LANES, class Op>
 __device__ inline float lanes_all(float x, const Op &op) {
   const auto from = [](float y, auto ctrl) {
@@ -206,16 +206,74 @@ __device__ inline float lanes_all(float x, const Op &op) {
   if (LANES >= 2) x = op(x, from(x, std::integral_constant<int, 0xB1>{}));    // quad_perm: the other of a pair
   if (LANES >= 4) x = op(x, from(x, std::integral_constant<int, 0x4E>{}));    // the other pair of a quad
   if (LANES >= 8) x = op(x, from(x, std::integral_constant<int, 0x141>{}));   // row_half_mirror: the other quad
+  if (LANES >= 16) x = op(x, from(x, std::integral_constant<int, 0x140>{}));  // row_mirror: the other eight
   return x;
+}
+
+// Largest logits and sums of exponentials of the groups of four vectors a thread, from vector v of the row on.
+template <int DT, int LANES, int T>
+__device__ void group_sums(const Row<DT> &row, const Stretch &all, uint32_t v, float c2, float (&m)[4], float (&s)[4]) {
+  constexpr int E = Num<DT>::E;
+  const auto larger = [](float x, float y) { return fmaxf(x, y); };
+  const auto plus = [](float x, float y) { return x + y; };
+  u32x4 w[4];
+  if (v + 4 * T <= all.b1) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) w[u] = row.load_once(v + u * T, threadIdx.x);
+  } else {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      w[u] = Num<DT>::masked();
+      if (v + u * T + threadIdx.x < all.b1) w[u] = row.load_once(v + u * T, threadIdx.x);
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    float x[E];
+    Num<DT>::widen(w[u], x);
+    m[u] = x[0];
+#pragma unroll
+    for (int i = 1; i < E; ++i) m[u] = fmaxf(m[u], x[i]);
+    m[u] = lanes_all<LANES>(m[u], larger);
+    const float ref2 = base2_ref(m[u], c2);
+    s[u] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < E; ++i) s[u] += base2_exp(x[i], c2, ref2);
+    s[u] = lanes_all<LANES>(s[u], plus);
+  }
+}
+
+// The groups of a row by many workgroups, a load of four vectors a thread each: largest logits and sums of row r at
+// `groups` + 2 * n_groups * r.
+template <int DT, int LANES>
+__global__ __launch_bounds__(kTopThreads) void logits_groups_kernel(TeacherArgs g, uint32_t n_groups, float *groups) {
+  constexpr int T = kTopThreads;
+  const uint64_t r = blockIdx.y;
+  if (g.a.weight && uniform_load(g.a.weight + r) == 0.0f) return;
+  const Row<DT> row(g.a.logits, r, g.a.row_stride, g.a.vocab);
+  const Stretch all(row, 0, row.nv);
+  const uint32_t v = blockIdx.x * 4 * T;
+  float m[4], s[4];
+  group_sums<DT, LANES, T>(row, all, all.b0 + v, g.c2, m, s);
+  float *at = groups + 2ull * n_groups * r;
+  if (threadIdx.x % LANES == 0) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const uint32_t id = (v + u * T + threadIdx.x) / LANES;
+      at[id] = m[u];
+      at[n_groups + id] = s[u];
+    }
+  }
 }
 
 // Rows by groups.  One pass finds every group's largest logit and its sum of exponentials (relative to that logit); at
 // least k logits reach the k-th largest of the groups' largest (or a little less), so only the few groups that reach
-// it are looked through again for candidates.  A group is LANES neighbouring vectors, up to a line of 128 bytes, so
-// that looking through it again moves no more than it holds (with groups of vectors 4 KB apart, 8192 x 131072 bf16,
+// it are looked through again for candidates.  A group is LANES neighbouring vectors, a line of 128 bytes or a part of one
+// (two lines in long rows), so that looking through it again moves no more than it holds (with groups of vectors 4 KB apart, 8192 x 131072 bf16,
 // k = 256, that moved a whole row again: 560 us).
 template <int DT, int LANES, int T>
-__global__ __launch_bounds__(T) void logits_topk_groups_kernel(TeacherArgs g, uint32_t n_groups, uint32_t cap, uint32_t region) {
+__global__ __launch_bounds__(T) void logits_topk_groups_kernel(TeacherArgs g, uint32_t n_groups, uint32_t cap, uint32_t region,
+                                                             const float *groups) {
   using K = Key<DT>;
   constexpr int E = Num<DT>::E;
   extern __shared__ __align__(16) uint8_t dyn[];
@@ -239,42 +297,27 @@ __global__ __launch_bounds__(T) void logits_topk_groups_kernel(TeacherArgs g, ui
   const uint32_t b0 = all.b0, b1 = all.b1;
   const float c2 = g.c2;
   float top = kNegInf;
-  const auto larger = [](float x, float y) { return fmaxf(x, y); };
-  const auto plus = [](float x, float y) { return x + y; };
-  for (uint32_t v = 0; v < n_groups * LANES; v += 4 * T) {
-    u32x4 w[4];
-    if (b0 + v + 4 * T <= b1) {
-#pragma unroll
-      for (int u = 0; u < 4; ++u) w[u] = row.load_once(b0 + v + u * T, threadIdx.x);
-    } else {
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        w[u] = Num<DT>::masked();
-        if (b0 + v + u * T + threadIdx.x < b1) w[u] = row.load_once(b0 + v + u * T, threadIdx.x);
-      }
+  if (groups) {   // (by logits_groups_kernel)
+    const float *at = groups + 2ull * n_groups * r;
+    for (uint32_t i = threadIdx.x; i < n_groups; i += T) {
+      const float m = at[i];
+      top = fmaxf(top, m);
+      gkey[i] = __float_as_uint(m);
+      gsum[i] = at[n_groups + i];
     }
-    float m[4], s[4];
+  } else {
+    for (uint32_t v = 0; v < n_groups * LANES; v += 4 * T) {
+      float m[4], s[4];
+      group_sums<DT, LANES, T>(row, all, b0 + v, c2, m, s);
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      float x[E];
-      Num<DT>::widen(w[u], x);
-      m[u] = x[0];
+      for (int u = 0; u < 4; ++u) top = fmaxf(top, m[u]);
+      if (threadIdx.x % LANES == 0) {
 #pragma unroll
-      for (int i = 1; i < E; ++i) m[u] = fmaxf(m[u], x[i]);
-      m[u] = lanes_all<LANES>(m[u], larger);
-      const float ref2 = base2_ref(m[u], c2);
-      s[u] = 0.0f;
-#pragma unroll
-      for (int i = 0; i < E; ++i) s[u] += base2_exp(x[i], c2, ref2);
-      s[u] = lanes_all<LANES>(s[u], plus);
-      top = fmaxf(top, m[u]);
-    }
-    if (threadIdx.x % LANES == 0) {
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const uint32_t id = (v + u * T + threadIdx.x) / LANES;
-        gkey[id] = __float_as_uint(m[u]);
-        gsum[id] = s[u];
+        for (int u = 0; u < 4; ++u) {
+          const uint32_t id = (v + u * T + threadIdx.x) / LANES;
+          gkey[id] = __float_as_uint(m[u]);
+          gsum[id] = s[u];
+        }
       }
     }
   }
@@ -592,33 +635,43 @@ __global__ __launch_bounds__(kTopThreads) void logits_topk_any_kernel(TeacherArg
 }
 
 template <int DT, int LANES, int T>
-static hipError_t run_groups(const TeacherArgs &g, uint32_t nv, hipStream_t stream) {
+static hipError_t run_groups(const TeacherArgs &g, uint32_t nv, uint8_t *ws, hipStream_t stream) {
   const uint32_t n_groups = (uint32_t)cdiv(nv, 4 * T) * 4 * T / LANES;   // (of whole loads)
   const uint32_t cap = 2 * (uint32_t)ru4(g.a.k) + 256;
-  // the groups' keys and sums, later the indices level with the k-th, then a bit a
-  // logit (in whole quads of words a thread)
+  // the groups' keys and sums, later the indices level with the k-th, then a bit a logit (in whole quads of words a
+  // thread)
   const uint32_t words = (uint32_t)cdiv((uint64_t)nv * Num<DT>::E, 128 * T) * 4 * T;
   uint32_t region = 8 * n_groups > 4 * words ? 8 * n_groups : 4 * words;
   if (region < 4 * cap) region = 4 * cap;
   const uint32_t dyn = region + 8 * cap + 2 * n_groups;
-  logits_topk_groups_kernel<DT, LANES, T><<<(uint32_t)g.a.rows, T, dyn, stream>>>(g, n_groups, cap, region);
+  float *groups = nullptr;
+  if (g.a.rows <= kFewRows && nv >= kLongVecs) {
+    // few long rows: their groups by workgroups for every compute unit, in a launch of their own
+    groups = reinterpret_cast<float *>(ws);
+    const uint32_t per = 4 * kTopThreads;
+    logits_groups_kernel<DT, LANES><<<dim3(n_groups * LANES / per, (uint32_t)g.a.rows), kTopThreads, 0, stream>>>(g, n_groups, groups);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  logits_topk_groups_kernel<DT, LANES, T><<<(uint32_t)g.a.rows, T, dyn, stream>>>(g, n_groups, cap, region, groups);
   return hipGetLastError();
 }
 
 // The largest groups of which there are still two or more for each entry (then some 1.4 candidates an entry pass);
 // never more than 4096.
 template <int DT, int T>
-static hipError_t run_lanes(const TeacherArgs &g, uint32_t nv, hipStream_t stream) {
-  if (nv >= 16 * g.a.k) return run_groups<DT, 8, T>(g, nv, stream);
-  if (nv >= 8 * g.a.k) return run_groups<DT, 4, T>(g, nv, stream);
-  if (nv >= 4 * g.a.k) return run_groups<DT, 2, T>(g, nv, stream);
-  return run_groups<DT, 1, T>(g, nv, stream);
+static hipError_t run_lanes(const TeacherArgs &g, uint32_t nv, uint8_t *ws, hipStream_t stream) {
+  if (nv > 32768) return run_groups<DT, 16, T>(g, nv, ws, stream);
+  if (nv >= 16 * g.a.k) return run_groups<DT, 8, T>(g, nv, ws, stream);
+  if (nv >= 8 * g.a.k) return run_groups<DT, 4, T>(g, nv, ws, stream);
+  if (nv >= 4 * g.a.k) return run_groups<DT, 2, T>(g, nv, ws, stream);
+  return run_groups<DT, 1, T>(g, nv, ws, stream);
 }
 
 template <int DT>
-static hipError_t run_typed(const TeacherArgs &g, hipStream_t stream) {
+static hipError_t run_typed(const TeacherArgs &g, uint8_t *ws, hipStream_t stream) {
   const uint32_t nv = row_vecs(g.a.vocab, DT, g.a.row_stride), k = g.a.k;
-  if (nv > kChunkVecs) {
+  if (nv > kGroupVecs || nv * Num<DT>::E > kGroupWords) {
     logits_topk_any_kernel<DT><<<(uint32_t)g.a.rows, kTopThreads, 0, stream>>>(g);
     return hipGetLastError();
   }
@@ -628,20 +681,19 @@ static hipError_t run_typed(const TeacherArgs &g, hipStream_t stream) {
   }
   // Rows that fill the device take 256 threads (512: 98 -> 119 us for 4096 x 50257 bf16), fewer than that 1024 (one row
   // of 50,257 f32 in 20 us with 256 threads), rows of a few loads one wave.
-  if (nv <= 512) return run_lanes<DT, 64>(g, nv, stream);
-  return g.a.rows >= 512 ? run_lanes<DT, 256>(g, nv, stream) : run_lanes<DT, 1024>(g, nv, stream);
+  if (nv <= 512) return run_lanes<DT, 64>(g, nv, ws, stream);
+  return g.a.rows >= 512 ? run_lanes<DT, 256>(g, nv, ws, stream) : run_lanes<DT, 1024>(g, nv, ws, stream);
 }
 
 hipError_t logits_topk(const DistillCall &call, uint8_t *out, uint8_t *ws, hipStream_t stream) {
-  (void)ws;
   TeacherArgs g{};
   g.a = call;
   g.c2 = (float)(1.44269504088896340736 / (double)call.temperature);
   g.out = out;
   switch (call.dtype) {
-    case BPC_F32: return run_typed<BPC_F32>(g, stream);
-    case BPC_F16: return run_typed<BPC_F16>(g, stream);
-    default: return run_typed<BPC_BF16>(g, stream);
+    case BPC_F32: return run_typed<BPC_F32>(g, ws, stream);
+    case BPC_F16: return run_typed<BPC_F16>(g, ws, stream);
+    default: return run_typed<BPC_BF16>(g, ws, stream);
   }
 }
 

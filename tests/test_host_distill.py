@@ -1,6 +1,8 @@
 """Distillation operators, what needs no GPU: sizes, refusals before the first HIP call, the binding's own checks,
 and the plain forms of the tests against each other (the gradient against differences)."""
 import ctypes as C
+import os
+import subprocess
 
 import numpy as np
 import pytest
@@ -112,6 +114,37 @@ def test_workspace_grows_with_rows(bpc):
                                                                  1000, 1024, 2047, 4096, 10000, 100000)]
             assert sizes[0] >= 256 and sizes == sorted(sizes)
             assert all(s % 256 == 0 for s in sizes)
+
+
+@pytest.fixture(scope="module")
+def geometry(tmp_path_factory):
+    """csrc/distill_geometry.hpp compiled for the host."""
+    so = str(tmp_path_factory.mktemp("distill") / "host_distill.so")
+    here = os.path.dirname(os.path.abspath(__file__))
+    subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-shared", "-fPIC", "-o", so, os.path.join(here, "host_distill.cpp")], check=True)
+    L = C.CDLL(so)
+    L.dg_needed.argtypes, L.dg_needed.restype = [C.c_uint64, C.c_uint32, C.c_int, C.c_uint64, C.c_int], C.c_uint64
+    L.dg_cut.argtypes = [C.c_uint64, C.c_uint32, C.c_int, C.c_uint64, C.c_int] + [C.c_void_p] * 3
+    return L
+
+
+def test_every_call_fits_its_workspace_and_its_rows(bpc, geometry):
+    rs = np.random.default_rng(1)
+    chunks, vecs, nv = (C.c_uint32() for _ in range(3))
+    for _ in range(3000):
+        vocab = int(np.exp(rs.uniform(0, np.log(1 << 24))))
+        rows = int(np.exp(rs.uniform(0, np.log((1 << 22) - 1))))
+        smaller = int(rs.integers(1, rows + 1))
+        size = bpc.distill_workspace_bytes(bpc.make_distill(bpc.TOPK, vocab, 8), rows)
+        for dtype in range(3):
+            for stride in (vocab, vocab + 1, (vocab + 63) // 64 * 64):
+                for step in (0, 1):
+                    for r in (rows, smaller, 1):
+                        assert geometry.dg_needed(r, vocab, dtype, stride, step) <= size
+                        geometry.dg_cut(r, vocab, dtype, stride, step, C.addressof(chunks), C.addressof(vecs), C.addressof(nv))
+                        assert chunks.value * vecs.value >= nv.value and chunks.value <= 65535
+                        if chunks.value > 1 or step:
+                            assert vecs.value <= 16384
 
 
 def test_binding_refuses_what_the_kernels_cannot_take(bpc, monkeypatch):
