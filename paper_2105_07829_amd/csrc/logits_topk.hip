@@ -177,6 +177,22 @@ __device__ uint32_t kth_key(const Count &count, uint32_t k, uint32_t lo, uint32_
   return lo;
 }
 
+// The same, beginning in steps down from the largest logit: a few are enough for logits of ordinary spread.
+template <class K, class Count>
+__device__ uint32_t kth_key_from_top(const Count &count, uint32_t k, float top, uint32_t slack, uint32_t *reach) {
+  uint32_t lo = K::kLowest, hi = K::of(top);
+  for (float x = 2.0f; x < 1e5f; x *= 2.0f) {
+    const uint32_t key = K::of(top - x);
+    if (key <= K::kLowest) break;
+    if (count(key) >= k) {
+      lo = key;
+      break;
+    }
+    hi = key - 1;
+  }
+  return kth_key(count, k, lo, hi, slack, reach);
+}
+
 // Adds up the waves' counts with one barrier a count: three counters take turns, each is cleared behind the barrier
 // after the one that it was read behind.  (All threads, a barrier before the first add and before the next Tally.)
 struct Tally {
@@ -356,18 +372,7 @@ __global__ __launch_bounds__(T) void logits_topk_groups_kernel(TeacherArgs g, ui
       }
       return tally.add(c);
     };
-    // (in steps down from the top first: a few are enough for logits of ordinary spread)
-    uint32_t from = K::kLowest, high = K::of(top);
-    for (float x = 2.0f; x < 1e5f; x *= 2.0f) {
-      const uint32_t key = K::of(top - x);
-      if (key <= K::kLowest) break;
-      if (count(key) >= g.a.k) {
-        from = key;
-        break;
-      }
-      high = key - 1;
-    }
-    low = kth_key(count, g.a.k, from, high, g.a.k / 8 + 4, &reach);
+    low = kth_key_from_top<K>(count, g.a.k, top, g.a.k / 8 + 4, &reach);
     if (low == 0) low = K::kLowest;
   }
   float rest = 0.0f;   // relative to 2^top2
@@ -549,10 +554,11 @@ constexpr uint32_t kDenseVocab = 15360;   // (60 KB)
 
 template <int DT>
 __global__ __launch_bounds__(kTopThreads) void logits_topk_dense_kernel(TeacherArgs g) {
-  constexpr int E = Num<DT>::E, T = kTopThreads;
+  using K = Key<DT>;
+  constexpr int E = Num<DT>::E, T = kTopThreads, WAVES = T / 64;
   extern __shared__ __align__(16) uint8_t dyn[];
-  __shared__ float lds[T / 64];
-  __shared__ uint32_t counters[3], scan_lds[T / 64];
+  __shared__ float lds[WAVES];
+  __shared__ uint32_t counters[3], above_of[WAVES], level_of[WAVES];
   const uint64_t r = blockIdx.x;
   uint8_t *rec = g.out + uniform_off(r * g.a.message_stride);
   if (g.a.weight && uniform_load(g.a.weight + r) == 0.0f) {
@@ -560,65 +566,82 @@ __global__ __launch_bounds__(kTopThreads) void logits_topk_dense_kernel(TeacherA
     return;
   }
   const Row<DT> row(g.a.logits, r, g.a.row_stride, g.a.vocab);
-  float *x = reinterpret_cast<float *>(dyn);
-  const uint32_t n = g.a.vocab;
+  // (keys as the vectors lie: logit j is number j + row.off, what is outside the row has key 0)
+  uint32_t *key = reinterpret_cast<uint32_t *>(dyn);
+  const uint32_t n = row.nv * E, quads = n / 4;
   float top = kNegInf;
-  bool nan = false;
+  bool odd = false;
   for (uint32_t v = threadIdx.x; v < row.nv; v += T) {
     float y[E];
     row.load_any(v, y);
+    uint4 *to = reinterpret_cast<uint4 *>(key + v * E);
+#pragma unroll
+    for (int i = 0; i < E; i += 4) to[i / 4] = uint4{K::of(y[i]), K::of(y[i + 1]), K::of(y[i + 2]), K::of(y[i + 3])};
 #pragma unroll
     for (int i = 0; i < E; ++i) {
-      const uint32_t j = v * E - row.off + i;
-      if (j < n) x[j] = y[i];
       top = fmaxf(top, y[i]);
-      nan = nan || y[i] != y[i];
+      odd = odd || y[i] != y[i];
     }
   }
   top = all_max<T>(top, lds);
-  if (__syncthreads_or(nan)) top = __builtin_nanf("");
-  const float ref = ref_of(top);
-  uint32_t reach;
-  Tally tally(counters);
-  const uint32_t rounds = (n + T - 1) / T;
-  const auto count = [&](uint32_t key) {
-    uint32_t c = 0;
-    for (uint32_t i = 0; i < rounds; ++i) {
-      const uint32_t j = threadIdx.x + i * T;
-      c += wave_count(j < n ? order_key(x[j]) : 0u, key);
-    }
-    return tally.add(c);
-  };
-  const uint32_t kth = kth_key(count, g.a.k, kLowestKey, order_key(top), 0, &reach);
-  // each thread a stretch of the row, of odd length (so that the threads of a wave are in different banks)
-  const uint32_t len = ((n + T - 1) / T) | 1u;
-  const uint32_t lo = threadIdx.x * len < n ? threadIdx.x * len : n, hi = lo + len < n ? lo + len : n;
-  uint32_t above = 0, same = 0;
-  for (uint32_t j = lo; j < hi; ++j) {
-    const uint32_t key = order_key(x[j]);
-    above += key > kth ? 1u : 0u;
-    same += key == kth && key != 0 ? 1u : 0u;
+  if (__syncthreads_or(odd || !(fabsf(top * g.c2) < kFarRef))) {   // a NaN, an infinity, numbers far from 0, nothing at all
+    select_any<DT, T>(g, row, rec);
+    return;
   }
-  uint32_t all_above, all;
-  uint32_t at = block_exclusive_scan<T>(above, scan_lds, &all_above);
-  const uint32_t same_before = block_exclusive_scan<T>(same, scan_lds, &all);
-  // of the logits level with the k-th the first `open` are listed
-  const uint32_t open = all_above < g.a.k ? g.a.k - all_above : 0;
-  at += same_before < open ? same_before : open;
-  uint32_t left = same_before < open ? open - same_before : 0;
+  uint32_t reach, kth;
+  {
+    Tally tally(counters);
+    const auto count = [&](uint32_t least) {
+      uint32_t c = 0;
+      for (uint32_t i = threadIdx.x; i < quads; i += T) {
+        const uint4 q = reinterpret_cast<const uint4 *>(key)[i];
+        c += wave_count(q.x, least) + wave_count(q.y, least) + wave_count(q.z, least) + wave_count(q.w, least);
+      }
+      return tally.add(c);
+    };
+    kth = kth_key_from_top<K>(count, g.a.k, top, 0, &reach);
+    if (kth == 0) kth = K::kLowest;   // (fewer than k: all of them)
+  }
+  // each wave a stretch of the row, 64 logits at a time: how many are above the k-th and level with it ...
+  const uint32_t wave = threadIdx.x / 64, lane = threadIdx.x & 63, stretch = (n + T - 1) / T * 64;
+  const uint32_t lo = wave * stretch < n ? wave * stretch : n, hi = lo + stretch < n ? lo + stretch : n;
+  uint32_t above = 0, level = 0;
+  for (uint32_t j = lo; j < hi; j += 64) {
+    const uint32_t x = j + lane < hi ? key[j + lane] : 0u;
+    above += (uint32_t)__popcll(__ballot(x > kth));
+    level += (uint32_t)__popcll(__ballot(x == kth));
+  }
+  if (lane == 0) {
+    above_of[wave] = above;
+    level_of[wave] = level;
+  }
+  __syncthreads();
+  uint32_t all_above = 0, all_level = 0, level_at = 0;
+  above = 0;
+#pragma unroll
+  for (uint32_t w = 0; w < WAVES; ++w) {
+    above += w < wave ? above_of[w] : 0u;
+    level_at += w < wave ? level_of[w] : 0u;
+    all_above += above_of[w];
+    all_level += level_of[w];
+  }
+  // ... of which the first `open` are listed; then where each goes
+  const uint32_t open = g.a.k - all_above;
+  uint32_t at = above + (level_at < open ? level_at : open);
+  const float top2 = base2_ref(top, g.c2);
   float rest = 0.0f;
-  for (uint32_t j = lo; j < hi; ++j) {
-    const uint32_t key = order_key(x[j]);
-    bool take = key > kth;
-    if (key == kth && key != 0 && left > 0) {
-      take = true;
-      --left;
-    }
-    if (take) put_entry(g, rec, at++, j, x[j] - ref);
-    else if (key != 0) rest += exp2_hw((x[j] - ref) * g.c2);
+  for (uint32_t j = lo; j < hi; j += 64) {
+    const uint32_t x = j + lane < hi ? key[j + lane] : 0u;
+    const uint64_t before = (1ull << lane) - 1, same = __ballot(x == kth);
+    const bool take = x > kth || (x == kth && level_at + (uint32_t)__popcll(same & before) < open);
+    const uint64_t taken = __ballot(take);
+    if (take) put_entry(g, rec, at + (uint32_t)__popcll(taken & before), j + lane - row.off, K::value(x) - top);
+    else if (x != 0) rest += base2_exp(K::value(x), g.c2, top2);
+    level_at += (uint32_t)__popcll(same);
+    at += (uint32_t)__popcll(taken);
   }
   rest = all_sum<T>(rest, lds);
-  close_record<T>(g, rec, all_above + (all < open ? all : open), rest, top);
+  close_record<T>(g, rec, all_above + (all_level < open ? all_level : open), rest * exp2_hw(-__builtin_fmaf(top, g.c2, -top2)), top);
 }
 
 // Rows of any length by the radix select alone.
@@ -676,7 +699,7 @@ static hipError_t run_typed(const TeacherArgs &g, uint8_t *ws, hipStream_t strea
     return hipGetLastError();
   }
   if (nv < 2 * k && g.a.vocab <= kDenseVocab) {
-    logits_topk_dense_kernel<DT><<<(uint32_t)g.a.rows, kTopThreads, 4 * g.a.vocab, stream>>>(g);
+    logits_topk_dense_kernel<DT><<<(uint32_t)g.a.rows, kTopThreads, 4 * nv * Num<DT>::E, stream>>>(g);
     return hipGetLastError();
   }
   // Rows that fill the device take 256 threads (512: 98 -> 119 us for 4096 x 50257 bf16), fewer than that 1024 (one row
