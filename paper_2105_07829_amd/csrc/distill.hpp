@@ -4,6 +4,7 @@
 #pragma once
 #include "device_utils.hpp"
 #include "distill_geometry.hpp"
+#include <type_traits>
 
 namespace bpc {
 
@@ -154,32 +155,52 @@ struct Stretch {
   }
 };
 
+// Over 2, 4, 8 or 16 neighbouring lanes, in all of them: moves inside a row of lanes cost no LDS access.
+template <int LANES, class Op>
+__device__ inline float lanes_all(float x, const Op &op) {
+  const auto from = [](float y, auto ctrl) {
+    return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(y), decltype(ctrl)::value, 0xf, 0xf, true));
+  };
+  if (LANES >= 2) x = op(x, from(x, std::integral_constant<int, 0xB1>{}));    // quad_perm: the other of a pair
+  if (LANES >= 4) x = op(x, from(x, std::integral_constant<int, 0x4E>{}));    // the other pair of a quad
+  if (LANES >= 8) x = op(x, from(x, std::integral_constant<int, 0x141>{}));   // row_half_mirror: the other quad
+  if (LANES >= 16) x = op(x, from(x, std::integral_constant<int, 0x140>{}));  // row_mirror: the other eight
+  return x;
+}
+
+struct Plus {
+  __device__ float operator()(float x, float y) const { return x + y; }
+};
+struct Larger {
+  __device__ float operator()(float x, float y) const { return fmaxf(x, y); }
+};
+template <class Op>
+__device__ inline float wave_all(float x, const Op &op) {
+  x = lanes_all<16>(x, op);
+  x = op(x, __shfl_xor(x, 16, 64));
+  return op(x, __shfl_xor(x, 32, 64));
+}
+// Over the values that the waves of a workgroup left in LDS, `apart` floats apart, in every thread.
+template <int WAVES, class Op>
+__device__ inline float waves_all(const float *v, int apart, const Op &op) {
+  static_assert(WAVES == 1 || WAVES == 4 || WAVES == 8 || WAVES == 16, "");
+  return lanes_all<WAVES>(v[(threadIdx.x % WAVES) * apart], op);
+}
+
 // Sum and maximum over a workgroup in a fixed order, in every thread.  `lds`: one float a wave.
-template <int THREADS>
-__device__ inline float all_sum(float x, float *lds) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
+template <int THREADS, class Op>
+__device__ inline float all_of(float x, float *lds, const Op &op) {
+  x = wave_all(x, op);
   if (THREADS == 64) return x;
   __syncthreads();
   if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
   __syncthreads();
-  float t = 0.0f;
-#pragma unroll
-  for (int w = 0; w < THREADS / 64; ++w) t += lds[w];
-  return t;
+  return waves_all<THREADS / 64>(lds, 1, op);
 }
 template <int THREADS>
-__device__ inline float all_max(float x, float *lds) {
-  x = wave_max(x);
-  if (THREADS == 64) return x;
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
-  __syncthreads();
-  float t = lds[0];
-#pragma unroll
-  for (int w = 1; w < THREADS / 64; ++w) t = fmaxf(t, lds[w]);
-  return t;
-}
+__device__ inline float all_sum(float x, float *lds) { return all_of<THREADS>(x, lds, Plus()); }
+template <int THREADS>
+__device__ inline float all_max(float x, float *lds) { return all_of<THREADS>(x, lds, Larger()); }
 
 // The fields of a row's record (the record of TOPK / TOPK16 with the mass of the rest and the row's
 // largest logit in the header).

@@ -217,11 +217,9 @@ struct Exchange {
   float v[T / 64][N + M];
   __device__ void all(float *sums, float *most) {   // (one barrier; each Exchange is used once)
 #pragma unroll
-    for (int i = 0; i < N; ++i)
+    for (int i = 0; i < N; ++i) sums[i] = wave_all(sums[i], Plus());
 #pragma unroll
-      for (int o = 32; o > 0; o >>= 1) sums[i] += __shfl_xor(sums[i], o, 64);
-#pragma unroll
-    for (int i = 0; i < M; ++i) most[i] = wave_max(most[i]);
+    for (int i = 0; i < M; ++i) most[i] = wave_all(most[i], Larger());
     if (T == 64) return;
     if ((threadIdx.x & 63) == 0) {
 #pragma unroll
@@ -231,19 +229,9 @@ struct Exchange {
     }
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      float t = 0.0f;
+    for (int i = 0; i < N; ++i) sums[i] = waves_all<T / 64>(&v[0][i], N + M, Plus());
 #pragma unroll
-      for (int w = 0; w < T / 64; ++w) t += v[w][i];
-      sums[i] = t;
-    }
-#pragma unroll
-    for (int i = 0; i < M; ++i) {
-      float t = v[0][N + i];
-#pragma unroll
-      for (int w = 1; w < T / 64; ++w) t = fmaxf(t, v[w][N + i]);
-      most[i] = t;
-    }
+    for (int i = 0; i < M; ++i) most[i] = waves_all<T / 64>(&v[0][N + i], N + M, Larger());
   }
 };
 

@@ -7,7 +7,6 @@
 // formed as a difference.
 #include "distill.hpp"
 #include "kernels.hpp"
-#include <type_traits>
 
 namespace bpc {
 
@@ -213,25 +212,10 @@ struct Tally {
 
 constexpr int kTopThreads = 256;
 
-// Largest value and sum over 2, 4, 8 or 16 neighbouring lanes, in all of them.
-template <int LANES, class Op>
-__device__ inline float lanes_all(float x, const Op &op) {
-  const auto from = [](float y, auto ctrl) {
-    return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(y), decltype(ctrl)::value, 0xf, 0xf, true));
-  };
-  if (LANES >= 2) x = op(x, from(x, std::integral_constant<int, 0xB1>{}));    // quad_perm: the other of a pair
-  if (LANES >= 4) x = op(x, from(x, std::integral_constant<int, 0x4E>{}));    // the other pair of a quad
-  if (LANES >= 8) x = op(x, from(x, std::integral_constant<int, 0x141>{}));   // row_half_mirror: the other quad
-  if (LANES >= 16) x = op(x, from(x, std::integral_constant<int, 0x140>{}));  // row_mirror: the other eight
-  return x;
-}
-
 // Largest logits and sums of exponentials of the groups of four vectors a thread, from vector v of the row on.
 template <int DT, int LANES, int T>
 __device__ void group_sums(const Row<DT> &row, const Stretch &all, uint32_t v, float c2, float (&m)[4], float (&s)[4]) {
   constexpr int E = Num<DT>::E;
-  const auto larger = [](float x, float y) { return fmaxf(x, y); };
-  const auto plus = [](float x, float y) { return x + y; };
   u32x4 w[4];
   if (v + 4 * T <= all.b1) {
 #pragma unroll
@@ -250,12 +234,12 @@ __device__ void group_sums(const Row<DT> &row, const Stretch &all, uint32_t v, f
     m[u] = x[0];
 #pragma unroll
     for (int i = 1; i < E; ++i) m[u] = fmaxf(m[u], x[i]);
-    m[u] = lanes_all<LANES>(m[u], larger);
+    m[u] = lanes_all<LANES>(m[u], Larger());
     const float ref2 = base2_ref(m[u], c2);
     s[u] = 0.0f;
 #pragma unroll
     for (int i = 0; i < E; ++i) s[u] += base2_exp(x[i], c2, ref2);
-    s[u] = lanes_all<LANES>(s[u], plus);
+    s[u] = lanes_all<LANES>(s[u], Plus());
   }
 }
 
@@ -702,9 +686,11 @@ static hipError_t run_typed(const TeacherArgs &g, uint8_t *ws, hipStream_t strea
     logits_topk_dense_kernel<DT><<<(uint32_t)g.a.rows, kTopThreads, 4 * nv * Num<DT>::E, stream>>>(g);
     return hipGetLastError();
   }
-  // Rows that fill the device take 256 threads (512: 98 -> 119 us for 4096 x 50257 bf16), fewer than that 1024 (one row
-  // of 50,257 f32 in 20 us with 256 threads), rows of a few loads one wave.
-  if (nv <= 512) return run_lanes<DT, 64>(g, nv, ws, stream);
+  // What follows the pass over a row costs every wave about the same, so short rows of few entries take one wave, where
+  // there are rows enough (64 / 256 threads: 16000 x 9000 bf16, k = 20, 90 / 149 us; 4096 x 30522 f16 65 / 74; f32 128 /
+  // 98; k = 300 191 / 120).  Others take 256 threads where they fill the device (512: 119 us for 98 of 4096 x 50257
+  // bf16), and 1024 where they do not (one row of 50,257 f32 20 us with 256).
+  if (nv <= 512 || (g.a.rows >= 512 && nv + 8 * k <= 4096)) return run_lanes<DT, 64>(g, nv, ws, stream);
   return g.a.rows >= 512 ? run_lanes<DT, 256>(g, nv, ws, stream) : run_lanes<DT, 1024>(g, nv, ws, stream);
 }
 
