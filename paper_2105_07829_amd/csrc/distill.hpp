@@ -15,6 +15,17 @@ constexpr float kNegInf = -__builtin_huge_valf();
 // 1 GiB of 2-byte elements, reads 8 %: reads are aligned here).
 typedef u32x4 u32x4_any __attribute__((aligned(2)));
 
+// Eight 16-bit elements of which those whose bit is set become -inf.
+__device__ inline u32x4 mask_halves(u32x4 v, uint32_t bits, uint32_t minus_inf) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_sbfe((int)bits, 2 * i, 1), hi = (uint32_t)__builtin_amdgcn_sbfe((int)bits, 2 * i + 1, 1);
+    const uint32_t m = __builtin_amdgcn_perm(hi, lo, 0x07060100u);
+    v[i] = (v[i] & ~m) | (minus_inf & m);
+  }
+  return v;
+}
+
 // One type of logits: E of them fill a 16-byte vector.
 template <int DT> struct Num;
 template <> struct Num<BPC_F32> {
@@ -25,6 +36,15 @@ template <> struct Num<BPC_F32> {
   }
   static __device__ u32x4 narrow(const float *x) { return as_u32x4(x[0], x[1], x[2], x[3]); }
   static __device__ u32x4 masked() { return u32x4{0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u}; }   // -inf
+  // The elements whose bit is set become -inf.
+  static __device__ u32x4 mask(u32x4 v, uint32_t bits) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t m = (uint32_t)__builtin_amdgcn_sbfe((int)bits, i, 1);
+      v[i] = (v[i] & ~m) | (0xff800000u & m);
+    }
+    return v;
+  }
   static __device__ float get(const raw *p) { return *p; }
   static __device__ void put(raw *p, float x) { *p = x; }
 };
@@ -53,6 +73,7 @@ template <> struct Num<BPC_F16> {
     return v;
   }
   static __device__ u32x4 masked() { return u32x4{0xfc00fc00u, 0xfc00fc00u, 0xfc00fc00u, 0xfc00fc00u}; }   // -inf
+  static __device__ u32x4 mask(u32x4 v, uint32_t bits) { return mask_halves(v, bits, 0xfc00fc00u); }
   static __device__ float get(const raw *p) { return (float)*p; }
   static __device__ void put(raw *p, float x) { *p = (_Float16)x; }
 };
@@ -79,6 +100,7 @@ template <> struct Num<BPC_BF16> {
     return v;
   }
   static __device__ u32x4 masked() { return u32x4{0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u}; }   // -inf
+  static __device__ u32x4 mask(u32x4 v, uint32_t bits) { return mask_halves(v, bits, 0xff80ff80u); }
   static __device__ float get(const raw *p) { return (float)*p; }
   static __device__ void put(raw *p, float x) { *p = (__bf16)x; }
 };

@@ -46,20 +46,23 @@ struct Marks {
     const uint32_t i = v - v0;
     return E == 8 ? bits[i] : (bits[i >> 1] >> (4 * (i & 1))) & 15u;
   }
-  // Marked words count as masked.  N vectors, `apart` apart, from v on; whether any word is marked.
+  // Marked words count as masked.  N vectors, `apart` apart, from v on.
   template <int N>
-  __device__ bool apply(uint32_t v, uint32_t apart, float *x) const {
-    if (!bits) return false;
+  __device__ void apply(uint32_t v, uint32_t apart, u32x4 *w) const {
+    if (!bits) return;
     uint32_t b[N], any = 0;
 #pragma unroll
     for (int u = 0; u < N; ++u) any |= b[u] = of(v + u * apart);
     if (any) {
 #pragma unroll
-      for (int u = 0; u < N; ++u)
-#pragma unroll
-        for (int k = 0; k < E; ++k) x[u * E + k] = (b[u] >> k) & 1 ? kNegInf : x[u * E + k];
+      for (int u = 0; u < N; ++u) w[u] = Num<DT>::mask(w[u], b[u]);
     }
-    return any != 0;
+  }
+  __device__ void apply_to(uint32_t v, float *x) const {
+    if (!bits) return;
+    const uint32_t b = of(v);
+#pragma unroll
+    for (int k = 0; k < E; ++k) x[k] = (b >> k) & 1 ? kNegInf : x[k];
   }
 };
 
@@ -145,7 +148,7 @@ __device__ void add_edges(const Row<DT> &row, const Stretch &st, const Marks<DT>
   if (st.edge(&v)) {
     float x[Num<DT>::E];
     row.load_any(v, x);
-    marks.template apply<1>(v, 0, x);
+    marks.apply_to(v, x);
     p->template add<HARD, Num<DT>::E>(x, c2);
   }
 }
@@ -176,20 +179,19 @@ __device__ FastSum scan(const Row<DT> &row, const Stretch &st, Four<DT, T> now, 
   uint32_t v = st.b0;
   while (v + 4 * T <= st.b1) {
     float x[4 * E];
+    marks.template apply<4>(v + threadIdx.x, T, now.w);
 #pragma unroll
     for (int u = 0; u < 4; ++u) Num<DT>::widen(now.w[u], x + u * E);
-    const uint32_t at = v;
     v += 4 * T;
     if (v < st.b1) now.load(row, st, v);   // (the next four are on their way)
-    marks.template apply<4>(at + threadIdx.x, T, x);
     p.add<HARD, 4 * E>(x, c2);
   }
 #pragma unroll
   for (int u = 0; u < 4; ++u) {
     if (v + u * T + threadIdx.x < st.b1) {
       float x[E];
+      marks.template apply<1>(v + u * T + threadIdx.x, 0, &now.w[u]);
       Num<DT>::widen(now.w[u], x);
-      marks.template apply<1>(v + u * T + threadIdx.x, 0, x);
       p.add<HARD, E>(x, c2);
     }
   }
@@ -203,7 +205,7 @@ __device__ PlainSum scan_plain(const Row<DT> &row, const Stretch &st, const Mark
   for (uint32_t v = st.b0 + threadIdx.x; v < st.b1; v += T) {
     float x[E];
     Num<DT>::widen(row.load(0, v), x);
-    marks.template apply<1>(v, 0, x);
+    marks.apply_to(v, x);
     p.add<HARD, E>(x, c2);
   }
   add_edges<DT, HARD>(row, st, marks, c2, &p);
@@ -252,20 +254,18 @@ struct Listed {
   float s_label;
   float rest;
 
-  // of the words [lo, hi) only (of every word the sums over a row need, of a stretch what its gradient needs)
+  // The record and the label ...
   template <bool HARD>
-  __device__ void read(const Args &g, const Row<DT> &row, uint64_t r, uint32_t lo, uint32_t hi) {
+  __device__ void request(const Args &g, uint64_t r) {
     const Record rec(g.a.messages, r, g.a.message_stride, g.a.k, g.a.half);
     n = rec.count(g.a.k);
     rest = g.a.rest_too ? rec.rest() : 0.0f;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       const uint32_t e = threadIdx.x + i * T;
-      idx[i] = kNone;
       if (e < g.a.k) {   // (the record has room for k entries: read before n is known)
-        const uint32_t j = rec.idx(e);
+        idx[i] = rec.idx(e);
         val[i] = rec.val(e);
-        idx[i] = e < n && j >= lo && j < hi ? j : kNone;
       }
     }
     label = kNone;
@@ -273,11 +273,22 @@ struct Listed {
       const int64_t l = g.a.labels[r];
       if (l >= 0 && l < (int64_t)g.a.vocab) label = (uint32_t)l;
     }
+  }
+  // ... and the student's logits of the words [lo, hi) among them (all words for the sums over a row, those of a stretch
+  // for its gradient: another stretch's gradient may just be written over the others).
+  __device__ void gather(const Row<DT> &row, uint32_t lo, uint32_t hi) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+      if (!(threadIdx.x + i * T < n && idx[i] >= lo && idx[i] < hi)) idx[i] = kNone;
 #pragma unroll
     for (int i = 0; i < PER; ++i)
       if (idx[i] != kNone) s[i] = Num<DT>::get(row.p + idx[i]);
-    // (not of another stretch, whose gradient may just be written over it)
     s_label = label != kNone && label >= lo && label < hi ? Num<DT>::get(row.p + label) : 0.0f;
+  }
+  template <bool HARD>
+  __device__ void read(const Args &g, const Row<DT> &row, uint64_t r, uint32_t lo, uint32_t hi) {
+    request<HARD>(g, r);
+    gather(row, lo, hi);
   }
   // Marks the words of the vectors [v0, v1); barriers inside.
   __device__ void mark(const Row<DT> &row, uint32_t v0, uint32_t v1, uint32_t *bits) const {
@@ -595,27 +606,27 @@ __global__ __launch_bounds__(T, WAVES) void distill_held_kernel(Args g) {
   }
   Listed<DT, T> list;
   list.template read<HARD != kNoHard>(g, row, r, 0, row.vocab);
+  float ends[E];
+  uint32_t end_v;
+  const bool has_end = grad.st.edge(&end_v);
+  if (has_end) row.load_any(end_v, ends);
   if (g.a.rest_too) list.mark(row, 0, row.nv, bits);
   const Marks<DT> marks{g.a.rest_too ? (const uint8_t *)bits : nullptr, 0};
   // largest unlisted logit; from here on the listed ones are -inf here (their gradients are written apart)
   float largest = kNegInf;
 #pragma unroll
   for (int i = 0; i < HOLD; ++i) {
-    const uint32_t v = b0 + i * T + threadIdx.x;
-    if (b0 + i * T < b1) {
+    const uint32_t v = b0 + i * T;
+    if (v < b1) {
+      if (v + threadIdx.x < b1) marks.template apply<1>(v + threadIdx.x, 0, &w[i]);
       float x[E];
       Num<DT>::widen(w[i], x);
-      if (v < b1 && marks.template apply<1>(v, 0, x)) w[i] = Num<DT>::narrow(x);
 #pragma unroll
       for (int e = 0; e < E; ++e) largest = fmaxf(largest, x[e]);
     }
   }
-  float ends[E];
-  uint32_t end_v;
-  const bool has_end = grad.st.edge(&end_v);
   if (has_end) {
-    row.load_any(end_v, ends);
-    marks.template apply<1>(end_v, 0, ends);
+    marks.apply_to(end_v, ends);
 #pragma unroll
     for (int e = 0; e < E; ++e) largest = fmaxf(largest, ends[e]);
   }
@@ -664,7 +675,10 @@ __global__ __launch_bounds__(T, WAVES) void distill_held_kernel(Args g) {
       }
     }
   }
-  grad.edges();
+  if (has_end) {
+    grad.one(ends);
+    grad.put_any(end_v, ends);
+  }
   grad.listed(g, list);
 }
 
