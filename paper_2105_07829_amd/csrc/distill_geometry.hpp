@@ -39,19 +39,19 @@ inline uint32_t row_vecs(uint32_t vocab, int dtype, uint64_t row_stride) {
 constexpr uint32_t kFewRows = 32, kLongVecs = 4096, kLeastVecs = 512, kFillChunks = 256;
 constexpr uint32_t kGradVecs = 16384;   // vectors of a row whose gradient one workgroup writes
 
-// How the sums over a row are formed: by one workgroup, or by one for each of its chunks and a launch that joins them.
-// One workgroup holds a bit a logit in LDS and, for loss and gradient in one call, the row in registers.
+// How the sums over a row are formed: by one workgroup, which keeps a bit a logit in LDS, or by one for each of its
+// chunks and a launch that joins them.
 struct Cut {
   uint32_t chunks;   // a row
-  uint32_t vecs;     // of a chunk, at most kChunkVecs
+  uint32_t vecs;     // of a chunk, at most kChunkVecs where there are several
 };
 constexpr uint32_t kMarkWords = 1u << 18;   // logits that have a bit in LDS
 inline Cut cut_rows(uint64_t rows, uint32_t vocab, int dtype, uint64_t row_stride, bool step) {
   const uint32_t nv = row_vecs(vocab, dtype, row_stride), e = 16 / elem_bytes(dtype);
-  const bool whole = step ? nv <= kChunkVecs : (uint64_t)nv * e <= kMarkWords;
-  // Few long rows of which only the loss is wanted are cut, too: 8 x 151,936 bf16 9.4 us cut and 16.1 whole, 1 x 50,257
-  // 9.0 and 10.4; 64 x 50,257 11.5 and 11.0.
-  if (whole && (step || rows > kFewRows || nv < kLongVecs)) return {1, nv};
+  const bool whole = (uint64_t)nv * e <= kMarkWords;
+  // Few long rows are cut, too.  Loss: 8 x 151,936 bf16 9.4 us cut and 16.1 whole, 1 x 50,257 9.0 and 10.4; 64 x 50,257
+  // 11.5 and 11.0.  Loss and gradient, in three launches: 10 x 262,144 f32 24.5 and 29.2, so only very long ones.
+  if (whole && (rows > kFewRows || nv < (step ? kChunkVecs + 1 : kLongVecs))) return {1, nv};
   uint64_t chunks = cdiv(kFillChunks, rows);   // for every compute unit
   const uint64_t most = cdiv(nv, kLeastVecs), least = cdiv(nv, kChunkVecs);
   chunks = chunks < most ? chunks : most;

@@ -154,26 +154,27 @@ __device__ void add_edges(const Row<DT> &row, const Stretch &st, const Marks<DT>
 }
 
 // Four vectors of a body a thread, T apart, from v on; what is past its end reads as masked.
-template <int DT, int T>
+template <int DT, int T, bool ONCE = true>
 struct Four {
   u32x4 w[4];
+  __device__ static u32x4 get(const Row<DT> &row, uint32_t v) { return ONCE ? row.load_once(v, threadIdx.x) : row.load(v, threadIdx.x); }
   __device__ void load(const Row<DT> &row, const Stretch &st, uint32_t v) {
     if (v + 4 * T <= st.b1) {
 #pragma unroll
-      for (int u = 0; u < 4; ++u) w[u] = row.load_once(v + u * T, threadIdx.x);
+      for (int u = 0; u < 4; ++u) w[u] = get(row, v + u * T);
     } else {
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         w[u] = Num<DT>::masked();
-        if (v + u * T + threadIdx.x < st.b1) w[u] = row.load_once(v + u * T, threadIdx.x);
+        if (v + u * T + threadIdx.x < st.b1) w[u] = get(row, v + u * T);
       }
     }
   }
 };
 
 // A thread's share of a stretch; `now`: the first four vectors, loaded by the caller before whatever else a row needs.
-template <int DT, int HARD, int T>
-__device__ FastSum scan(const Row<DT> &row, const Stretch &st, Four<DT, T> now, const Marks<DT> &marks, float c2) {
+template <int DT, int HARD, int T, bool ONCE>
+__device__ FastSum scan(const Row<DT> &row, const Stretch &st, Four<DT, T, ONCE> now, const Marks<DT> &marks, float c2) {
   constexpr int E = Num<DT>::E;
   FastSum p;
   uint32_t v = st.b0;
@@ -575,6 +576,38 @@ __global__ __launch_bounds__(T) void distill_loss_kernel(Args g) {
   put_stats(g, r, st);
 }
 
+// Whole rows, a workgroup each, loss and gradient in two passes: the second finds the row in the last-level cache.
+template <int DT, int HARD, int T, int WAVES>
+__global__ __launch_bounds__(T, WAVES) void distill_twice_kernel(Args g) {
+  extern __shared__ uint32_t bits[];   // (TAIL_REST)
+  __shared__ FinishLds<T> lds;
+  const uint64_t r = blockIdx.x;
+  const Row<DT> row(g.a.logits, r, g.a.row_stride, g.a.vocab);
+  const float weight = weight_of(g, r);
+  Gradient<DT, HARD, T> grad(g, row, r, 0, row.nv);
+  if (weight == 0.0f) {
+    if (threadIdx.x == 0) g.a.loss[r] = 0.0f;
+    grad.zero();
+    return;
+  }
+  Four<DT, T, false> first;
+  first.load(row, grad.st, grad.st.b0);
+  Listed<DT, T> list;
+  list.template read<HARD != kNoHard>(g, row, r, 0, row.vocab);
+  if (g.a.rest_too) list.mark(row, 0, row.nv, bits);
+  const Marks<DT> marks{g.a.rest_too ? (const uint8_t *)bits : nullptr, 0};
+  const FastSum f = scan<DT, HARD, T>(row, grad.st, first, marks, g.c2);
+  const auto settle = [&](float m) { return settled<DT, HARD, T>(f, m, row, grad.st, marks, g.c2); };
+  const Stats st = finish<DT, HARD, T>(g, list, f.m, settle, weight, g.a.loss + r, lds);
+  Four<DT, T> again;
+  again.load(row, grad.st, grad.st.b0);
+  grad.prepare(g, weight, st, list);
+  __syncthreads();   // (every listed logit has been read)
+  grad.stream(again);
+  grad.edges();
+  grad.listed(g, list);
+}
+
 // Whole rows, a workgroup each, loss and gradient: the row stays in registers, HOLD vectors a thread, all of them
 // requested before anything else.
 template <int DT, int HARD, int T, int HOLD, int WAVES>
@@ -795,19 +828,27 @@ template <int DT, int HARD>
 static hipError_t run_typed(Args g, DistillRole role, uint8_t *ws, hipStream_t stream) {
   const uint32_t rows = (uint32_t)g.a.rows, nv = row_vecs(g.a.vocab, DT, g.a.row_stride);
   const Cut cut = cut_rows(g.a.rows, g.a.vocab, DT, g.a.row_stride, role == DistillRole::step);
+  const uint32_t marks_lds = g.a.rest_too ? (uint32_t)cdiv((uint64_t)nv * Num<DT>::E, 32) * 4 : 0;
   if (role == DistillRole::loss && cut.chunks == 1) {
-    const uint32_t dyn = g.a.rest_too ? (uint32_t)cdiv((uint64_t)nv * Num<DT>::E, 32) * 4 : 0;
-    if (nv <= 1024 && g.a.k <= kOneWaveK) distill_loss_kernel<DT, HARD, 64><<<rows, 64, dyn, stream>>>(g);
-    else if (rows >= 512) distill_loss_kernel<DT, HARD, 256><<<rows, 256, dyn, stream>>>(g);
-    else distill_loss_kernel<DT, HARD, 1024><<<rows, 1024, dyn, stream>>>(g);
+    // (4096 x 50257 bf16 with 256 / 512 / 1024 threads: 68 / 77 / 153 us, what a row costs beside its logits is the same
+    // for each; fewer rows than fill the device take as many threads as there are)
+    if (nv <= 1024 && g.a.k <= kOneWaveK) distill_loss_kernel<DT, HARD, 64><<<rows, 64, marks_lds, stream>>>(g);
+    else if (rows >= 512) distill_loss_kernel<DT, HARD, 256><<<rows, 256, marks_lds, stream>>>(g);
+    else distill_loss_kernel<DT, HARD, 1024><<<rows, 1024, marks_lds, stream>>>(g);
     return hipGetLastError();
   }
   if (role == DistillRole::step && cut.chunks == 1) {
+    // Held where two rows or more fit the registers of a compute unit and there are rows enough: 4096 x 50257 bf16 176 us
+    // held and 199 in two passes, 2048 x 30522 f16 56 and 80, 2000 x 32000 f32 97 and 119.  One row at a time leaves
+    // the memory idle while its sums are joined: 8192 x 131072 bf16 1023 held, 951 in two passes (three rows at a
+    // time).  Few rows: 100 x 30000 bf16 12.9 and 11.0, 61 x 128000 23.2 and 20.5.
     if (nv <= 512 && g.a.k <= kOneWaveK) return held_rows<DT, HARD, 64, 8, 4>(g, stream);
     if (nv <= 2048) return held_rows<DT, HARD, 256, 8, 5>(g, stream);
-    if (nv <= 4096) return held_rows<DT, HARD, 256, 16, 4>(g, stream);
-    if (nv <= 8192) return held_rows<DT, HARD, 512, 16, 4>(g, stream);
-    return held_rows<DT, HARD, 1024, 16, 4>(g, stream);
+    if (nv <= 4096 && rows >= 512) return held_rows<DT, HARD, 256, 16, 4>(g, stream);
+    if (nv <= 8192 && rows >= 512) return held_rows<DT, HARD, 512, 16, 4>(g, stream);
+    if (rows >= 512) distill_twice_kernel<DT, HARD, 512, 6><<<rows, 512, marks_lds, stream>>>(g);
+    else distill_twice_kernel<DT, HARD, 1024, 4><<<rows, 1024, marks_lds, stream>>>(g);
+    return hipGetLastError();
   }
   if (role != DistillRole::grad) {
     const DistillWs lay = distill_ws(g.a.rows, cut);

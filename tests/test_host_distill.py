@@ -143,8 +143,10 @@ def test_every_call_fits_its_workspace_and_its_rows(bpc, geometry):
                         assert geometry.dg_needed(r, vocab, dtype, stride, step) <= size
                         geometry.dg_cut(r, vocab, dtype, stride, step, C.addressof(chunks), C.addressof(vecs), C.addressof(nv))
                         assert chunks.value * vecs.value >= nv.value and chunks.value <= 65535
-                        if chunks.value > 1 or step:
+                        if chunks.value > 1:
                             assert vecs.value <= 16384
+                        else:   # a bit a logit in 32 KB
+                            assert nv.value * (4 if dtype == 0 else 8) <= 1 << 18
 
 
 def test_binding_refuses_what_the_kernels_cannot_take(bpc, monkeypatch):
