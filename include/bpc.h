@@ -1,6 +1,7 @@
 /*
  * bpc.h -- C ABI of the two-way error-feedback gradient-compression hot path
- * for one AMD MI355X (gfx950).
+ * for one AMD MI355X (gfx950), and of distillation from a teacher's logits that
+ * are sent as top-k messages (further down).
  *
  * The library implements, on one GPU, the arithmetic of the paper's gradient
  * aggregation with compression and error feedback (Algorithm 4), its variant
@@ -361,7 +362,7 @@ bpc_status_t bpc_adaptive_update(const bpc_params_t *params,
  *     n <= k   entries listed: the k largest logits of the row, ties to the lowest
  *              index, a NaN above +inf; -inf (a masked logit) is never listed
  *     top      the row's largest logit (-inf where n = 0)
- *     idx      strictly ascending; -1 from n to k
+ *     idx      strictly ascending; -1 from n to k (-0 and +0 are the same number)
  *     val      logit - top (TOPK16: as IEEE binary16, round to nearest even); -inf
  *              from n to k
  *     rest     sum over the logits not listed of exp((logit - top) / temperature)
@@ -387,7 +388,8 @@ bpc_status_t bpc_adaptive_update(const bpc_params_t *params,
  *   - Masked student logits (-inf) have probability and gradient 0; if the teacher
  *     gives such a word (or, with TAIL_REST, a rest that is masked as a whole) mass,
  *     the loss is +inf and the gradient of the listed words still -q_i.
- *   - A NaN or +inf among a row's logits makes that row's loss and gradient NaN.
+ *   - A NaN or +inf among a row's logits makes that row's loss and gradient NaN.  In a
+ *     teacher's row it makes values of its record NaN, and so the student's.
  * Unlike the gradient path these calls take infinities and NaN as described.  Sums are
  * formed in f32 in a fixed order: the same inputs give the same bits (in rows that start
  * elsewhere in their 128-byte line, or of another number, sums may be formed in another order).

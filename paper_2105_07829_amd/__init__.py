@@ -1,5 +1,5 @@
-"""Python binding of libbpc (include/bpc.h): two-way error-feedback gradient compression
-on one MI355X.
+"""Python binding of libbpc (include/bpc.h): two-way error-feedback gradient compression and
+distillation from a teacher's top logits on one MI355X.
 
 Argument marshalling only: every function takes torch tensors that live on the GPU, passes
 their ``data_ptr()`` and the current HIP stream through the C ABI, and raises ``BpcError``
@@ -386,6 +386,8 @@ def _logits(t, d, at, what="logits"):
 
 def _flat(t, dtype, n, at, what):
     """Pointer of a contiguous tensor of at least ``n`` elements on the current device."""
+    if t is None:
+        raise ValueError(f"{what} missing")
     if t.dtype is not dtype or t.numel() < n or not t.is_contiguous():
         raise ValueError(f"{what}: expected a contiguous {dtype} tensor of at least {n} elements, got {tuple(t.shape)} {t.dtype}")
     if t.get_device() != at or at < 0:

@@ -73,7 +73,7 @@ def workspace(bpc, d, rows):
     return torch.full((bpc.distill_workspace_bytes(d, rows),), 0xA5, dtype=torch.uint8, device="cuda")
 
 
-def check_topk(bpc, d, x, dtype, pad=0, weight=None):
+def check_topk(bpc, d, x, dtype, pad=0, weight=None, only=None):
     import torch
     rows, vocab = x.shape
     _, view = rows_of(x, dtype, pad)
@@ -86,7 +86,7 @@ def check_topk(bpc, d, x, dtype, pad=0, weight=None):
     assert bool((guard[size:] == 0x5A).all())
     n, idx, val, rest, top = fields(bpc, d, guard, rows)
     t = host(view)
-    for r in range(rows):
+    for r in (range(rows) if only is None else only):
         row = t[r] if weight is None or weight[r] != 0 else np.full(vocab, -np.inf, np.float32)
         want_idx, want_val, want_top, want_rest, bound = ref.topk_row(row, d.k, d.temperature, d.kind == bpc.TOPK16)
         assert n[r] == len(want_idx), (r, n[r], len(want_idx))
@@ -175,6 +175,17 @@ def test_topk_many_rows(bpc, dtype):
 
 
 @pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("vocab,k", [(20011, 20), (40001, 300), (140001, 64), (40001, 1024)])
+def test_topk_many_long_rows(bpc, dtype, vocab, k):
+    """The forms that rows of these lengths take where there are enough of them; some rows are looked at."""
+    x = np.random.default_rng(k).standard_normal((530, vocab), dtype=np.float32) * 2
+    hard = np.stack([row for _, row in shapes_of_rows(vocab)])
+    x[100:100 + len(hard)] = hard
+    check_topk(bpc, bpc.make_distill(bpc.TOPK, vocab, k, temperature=1.5), x, dtype, pad=3,
+               only=[0, 1, 2, 3, *range(100, 100 + len(hard)), 255, 256, 528, 529])
+
+
+@pytest.mark.parametrize("dtype", DT)
 def test_topk_lowest_of_the_type(bpc, dtype):
     import torch
     low = torch.finfo(tdtype(dtype)).min
@@ -214,7 +225,7 @@ def make_case(rs, vocab, k, rows, masked=0):
     return x, records
 
 
-def check_student(bpc, d, x, records, dtype, pad=0, gpad=None, labels=None, weight=None, in_place=False, want_nan=()):
+def check_student(bpc, d, x, records, dtype, pad=0, gpad=None, labels=None, weight=None, in_place=False, want_nan=(), only=None):
     import torch
     rows, vocab = x.shape
     buf, view = rows_of(x, dtype, pad)
@@ -258,7 +269,7 @@ def check_student(bpc, d, x, records, dtype, pad=0, gpad=None, labels=None, weig
     for loss, gbuf, grad in got:
         assert bool((loss[rows:] == 7.0).all()) and bool((gbuf[:, vocab:] == 7.0).all())
         l, g = host(loss), host(grad)
-        for r in range(rows):
+        for r in (range(rows) if only is None else only):
             if r in want_nan and wh[r] != 0.0:
                 assert np.isnan(l[r]) and np.isnan(g[r]).all(), r
                 continue
@@ -323,6 +334,26 @@ def test_student_many_rows(bpc, dtype, hard, tau, tail):
     weight = np.where(np.arange(1030) % 9 == 8, 0.0, 1.0)
     check_student(bpc, describe(bpc, vocab, 300, tail=tail, temperature=tau, hard_weight=hard), x, records, dtype, 1, 1,
                   list(rs.integers(0, vocab, 1030)), weight, want_nan=(3, 4))
+
+
+@pytest.mark.parametrize("vocab,dtype,hard,tau,tail", [(20011, "bf16", 0.2, 2.0, 1), (20011, "f16", 0.0, 1.0, 0), (50257, "bf16", 0.1, 1.3, 1),
+                                                       (30522, "f32", 0.1, 1.0, 1), (70001, "bf16", 0.3, 4.0, 1), (70001, "f32", 0.0, 0.7, 0)])
+def test_student_many_long_rows(bpc, vocab, dtype, hard, tau, tail):
+    """The forms that rows of these lengths take where there are enough of them; some rows are looked at."""
+    rs = np.random.default_rng(vocab)
+    rows, k = 530, 90
+    x = rs.standard_normal((rows, vocab), dtype=np.float32) * 2
+    idx = [np.sort(rs.choice(vocab, k, replace=False)) for _ in range(rows)]
+    records = [(k, i, -np.arange(k) * 0.07, 0.2, 3.0) for i in idx]
+    for r in range(rows):
+        x[r, idx[r]] += 5.0
+    x[20] = np.nan
+    x[40] *= 1e4
+    x[60, vocab // 2:] = -np.inf
+    weight = np.where(np.arange(rows) % 7 == 5, 0.0, 1.5)
+    labels = [int(idx[r][3]) if r % 3 else int(rs.integers(vocab)) for r in range(rows)]
+    check_student(bpc, describe(bpc, vocab, k, bpc.TOPK16, tail=tail, temperature=tau, hard_weight=hard), x, records, dtype, 1, 1,
+                  labels, weight, in_place=True, want_nan=(20,), only=[0, 1, 5, 20, 40, 60, 61, 255, 256, 511, 512, 528, 529])
 
 
 @pytest.mark.parametrize("tail", [0, 1])
