@@ -383,8 +383,8 @@ bpc_status_t bpc_adaptive_update(const bpc_params_t *params,
  *   - TAIL_DROP renormalises the teacher over its listed words; TAIL_REST compares
  *     the mass of all others as one more word.
  *   - A row of row_weight 0 has loss 0 and a gradient of zeros, its logits are not read.
- *   - A record with n = 0 gives no soft term, a label outside [0, vocab) (or labels
- *     NULL, or hard_weight 0) no hard term.
+ *   - A record with n = 0 (or soft_weight 0) gives no soft term, a label outside
+ *     [0, vocab) (or labels NULL, or hard_weight 0) no hard term.
  *   - Masked student logits (-inf) have probability and gradient 0; if the teacher
  *     gives such a word (or, with TAIL_REST, a rest that is masked as a whole) mass,
  *     the loss is +inf and the gradient of the listed words still -q_i.
@@ -449,8 +449,8 @@ bpc_status_t bpc_distill_loss(const bpc_distill_t *d, const void *logits, bpc_dt
  *   row_weight  as above; to carry on a gradient g_r of loss_r, pass row_weight_r * g_r.
  *               A row whose weight was 0 in bpc_distill_loss() has no statistics: its
  *               weight must be 0 here too.  soft_weight and hard_weight may differ from
- *               those of bpc_distill_loss(), except that a hard_weight that was 0 there
- *               must be 0 here; everything else in `d` must be the same.
+ *               those of bpc_distill_loss(), except that one that was 0 there must be 0
+ *               here; everything else in `d` must be the same.
  *   grad        device, `rows` rows of `vocab` elements of `dtype`, row r at element
  *               r * grad_stride, written; may be the logits themselves
  *               (grad == logits and grad_stride == row_stride), otherwise must not overlap them
@@ -461,8 +461,9 @@ bpc_status_t bpc_distill_grad(const bpc_distill_t *d, const void *logits, bpc_dt
                               void *grad, uint64_t grad_stride, void *hip_stream);
 
 /*
- * Student: loss and gradient in one call; the logits are read once where a workgroup
- * can hold a row.  Arguments as above.
+ * Student: loss and gradient in one call; the logits are read once where a compute unit
+ * can hold two rows or more, and again while they are in the last-level cache
+ * elsewhere.  Arguments as above.
  */
 bpc_status_t bpc_distill_step(const bpc_distill_t *d, const void *logits, bpc_dtype_t dtype,
                               uint64_t row_stride, uint64_t rows, const void *messages,

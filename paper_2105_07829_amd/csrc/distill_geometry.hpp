@@ -36,7 +36,10 @@ inline uint32_t row_vecs(uint32_t vocab, int dtype, uint64_t row_stride) {
   return (uint32_t)cdiv(vocab + (row_stride % e ? e - 1 : 0), e);
 }
 
-constexpr uint32_t kFewRows = 32, kLongVecs = 4096, kLeastVecs = 512, kFillChunks = 256;
+constexpr uint32_t kFewRows = 32;       // most rows of a call that are cut though a workgroup could have each whole,
+constexpr uint32_t kLongVecs = 4096;    // ... from this length on, in vectors,
+constexpr uint32_t kLeastVecs = 512;    // ... into chunks of at least this,
+constexpr uint32_t kFillChunks = 256;   // ... until every compute unit has one (512 or 1024: the same within 2 %)
 constexpr uint32_t kGradVecs = 16384;   // vectors of a row whose gradient one workgroup writes
 
 // How the sums over a row are formed: by one workgroup, which keeps a bit a logit in LDS, or by one for each of its

@@ -10,6 +10,15 @@
 // and the pass takes the whole row).  The gradient of an unlisted word is
 //   w exp((s_j - m_R) c) a c [exp((m_R - m) c) / Z - q_R / R] + w b exp(s_j - m_R) exp(m_R - m) / H,
 // two coefficients a row; the listed words and the label are written apart, after the others.
+//
+// What bounds it: the loss reads 2 or 4 bytes a logit for 7 to 9 vector instructions, so 4096 x 50257
+// bf16 with hard labels (68 us, 353 MB) is bound by vector issue (88 % busy) and smaller calls by the
+// chain record -> listed logits -> sums -> logarithms of a row; the gradient (136 us, 765 MB, 5.6 TB/s) by
+// the memory.  Both in one call: rows of which a compute unit holds two or more stay in registers (2048 x
+// 30522 f16 54 us for 225 MB), longer ones are read twice, the second time from the last-level cache (8192 x
+// 131072 bf16 953 us for 4.3 GB).  Not kept, measured on that last case: workgroups that take row after
+// row and load the next row while they write a gradient (1140 us: all of them read and write at the same
+// time); listed logits and gradients passed through a table in LDS instead of a gather and a scatter (1178).
 #pragma once
 #include "distill.hpp"
 #include "kernels.hpp"
@@ -359,7 +368,7 @@ __device__ Stats finish(const Args &g, const Listed<DT, T> &list, float largest,
     }
   }
   lds.sums.all(sums, nullptr);
-  const float q = list.n == 0 ? 0.0f : sums[2] + list.rest;
+  const float q = list.n == 0 || g.a.soft == 0.0f ? 0.0f : sums[2] + list.rest;   // 0: no soft term
   const float down = ref_of(most[0]) - ref;   // from the reference of the unlisted words to that of the row
   const float scale = most[0] == kNegInf ? 0.0f : exp2_hw(down * g.c2), scale1 = most[0] == kNegInf ? 0.0f : exp2_hw(down * kLog2e);
   // (nothing unlisted: the sums are 0 whatever the scale)

@@ -1,10 +1,16 @@
 // Teacher side of the distillation from top logits: the k largest logits of every row, in index
 // order, and the mass of all others (record format in include/bpc.h).
 //
-// Logits are ordered by 32-bit keys (order_key): the k-th largest key comes from a radix select,
-// whatever the row looks like; of the logits level with it the first ones are listed, by a prefix
-// sum over the row in index order.  The mass of the rest is summed over the unlisted logits, never
-// formed as a difference.
+// Logits are ordered by integer keys.  The usual form passes over a row once, in groups of a line of 128 bytes: the
+// k-th largest of the groups' largest logits bounds the row's k-th largest from below, and only groups that reach that
+// bound are looked through for candidates, of which a bisection finds the k-th.  Short rows of which a good part is
+// listed stay in LDS as keys; rows of NaN, infinities, numbers far from 0 or more candidates than there is room for go
+// through a radix select, which is right for every row.  Of the logits level with the k-th the first ones are listed.
+// The mass of the rest is summed over the unlisted logits, never formed as a difference.
+//
+// What bounds it: vector issue.  A logit takes 6 to 7 instructions in the pass and about as much again for what follows
+// it (bisections, second look, index order): 8192 x 131072 bf16, k = 256, 447 us (95 % busy; the pass alone 346 us, 6.2
+// TB/s), 4096 x 50257, k = 64, 97 us (83 %; the pass 63).
 #include "distill.hpp"
 #include "kernels.hpp"
 
@@ -50,7 +56,8 @@ __device__ inline void put_entry(const TeacherArgs &g, uint8_t *rec, uint32_t e,
   else reinterpret_cast<float *>(v)[e] = val;
 }
 
-// A whole row by a radix select: four passes for the key, one to write.  Right for every row.
+// A whole row by a radix select: four passes for the key, one to write.  Right for every row.  (8192 x 131072 bf16 3486
+// us: 256 counters in LDS take turns for logits of a few exponents.)
 template <int DT, int THREADS>
 __device__ void select_any(const TeacherArgs &g, const Row<DT> &row, uint8_t *rec) {
   constexpr int E = Num<DT>::E;
@@ -269,8 +276,9 @@ __global__ __launch_bounds__(kTopThreads) void logits_groups_kernel(TeacherArgs 
 // Rows by groups.  One pass finds every group's largest logit and its sum of exponentials (relative to that logit); at
 // least k logits reach the k-th largest of the groups' largest (or a little less), so only the few groups that reach
 // it are looked through again for candidates.  A group is LANES neighbouring vectors, a line of 128 bytes or a part of one
-// (two lines in long rows), so that looking through it again moves no more than it holds (with groups of vectors 4 KB apart, 8192 x 131072 bf16,
-// k = 256, that moved a whole row again: 560 us).
+// (two lines in long rows), so that looking through it again moves no more than it holds.  (8192 x 131072 bf16, k = 256:
+// with groups of vectors 4 KB apart the second look moved a whole row, 560 us against 531 at that time; with half lines
+// 535 us against 447, more groups to search and fewer workgroups a compute unit.)
 template <int DT, int LANES, int T>
 __global__ __launch_bounds__(T) void logits_topk_groups_kernel(TeacherArgs g, uint32_t n_groups, uint32_t cap, uint32_t region,
                                                              const float *groups) {

@@ -68,7 +68,7 @@ def student_row(s, n, idx, val, rest, tau, soft, hard, tail_rest, label, weight,
         e = np.exp(v * c)
         r = float(rest) if tail_rest else 0.0
         Q = e.sum() + r
-        soft_on = n > 0 and Q != 0.0
+        soft_on = n > 0 and Q != 0.0 and soft != 0.0
         kl, kl_err = 0.0, 0.0
         d_sum = (chain(V) + 4) * U + float((p[p > 0] * exp_error(logp[p > 0] * LOG2E)).sum()) + 2 * U
         g = np.zeros(V)

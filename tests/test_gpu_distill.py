@@ -382,6 +382,17 @@ def test_student_masks(bpc, vocab, tail):
                           3, 3, labels, in_place=True)
 
 
+def test_student_without_a_soft_term(bpc):
+    """soft_weight 0: the hard term alone, whatever the teacher says of words that the student masks."""
+    rs = np.random.default_rng(15)
+    for vocab in (700, 20000, 140000):
+        x, records = make_case(rs, vocab, 9, 3)
+        x[1, records[1][1][2]] = -np.inf
+        for tail in (0, 1):
+            check_student(bpc, describe(bpc, vocab, 9, tail=tail, temperature=3.0, soft_weight=0.0, hard_weight=1.0), x, records, "f32",
+                          labels=[3, 4, vocab - 1], in_place=True)
+
+
 def test_student_rest_far_below(bpc):
     """The teacher's rest is compared with a student's rest of 1e-87: a difference 1 - sum p would be 0."""
     rs = np.random.default_rng(8)
