@@ -872,11 +872,14 @@ static hipError_t run_typed(Args g, DistillRole role, uint8_t *ws, hipStream_t s
     e = hipGetLastError();
     if (e != hipSuccess || role == DistillRole::loss) return e;
   }
-  // (as many threads as a row keeps busy: the fewer rows are on their way at a time, the better the memory takes the
-  // writes; 4096 rows of 50,257 bf16, whose loss takes 68 us, 229 / 218 / 209 us for both with 256 / 512 / 1024)
+  // As many threads as a row keeps busy: the fewer rows are on their way at a time, the better the memory takes the
+  // writes (4096 x 50,257 bf16, whose loss takes 68 us, 229 / 218 / 209 us for both with 256 / 512 / 1024 threads).
+  // Short rows where there are many of them take fewer, for what a row costs beside its logits (loss and gradient of
+  // 16000 x 1000 bf16 46 us with 64 threads and 65 with 256, of 4000 x 10000 56 with 256 and 64 with 1024).
   g.vecs = kGradVecs;
   const dim3 grid(rows, (uint32_t)cdiv(nv, kGradVecs));
-  if (nv <= 512) distill_grad_kernel<DT, HARD, 256><<<grid, 256, 0, stream>>>(g);
+  if (nv <= 512 && g.a.k <= kOneWaveK) distill_grad_kernel<DT, HARD, 64><<<grid, 64, 0, stream>>>(g);
+  else if (nv <= 512 || (nv <= 2048 && rows >= 512)) distill_grad_kernel<DT, HARD, 256><<<grid, 256, 0, stream>>>(g);
   else distill_grad_kernel<DT, HARD, 1024><<<grid, 1024, 0, stream>>>(g);
   return hipGetLastError();
 }

@@ -676,7 +676,8 @@ static hipError_t run_groups(const TeacherArgs &g, uint32_t nv, uint8_t *ws, hip
 // never more than 4096.
 template <int DT, int T>
 static hipError_t run_lanes(const TeacherArgs &g, uint32_t nv, uint8_t *ws, hipStream_t stream) {
-  if (nv > 32768) return run_groups<DT, 16, T>(g, nv, ws, stream);
+  if constexpr (T != 64)   // (one wave takes short rows only)
+    if (nv > 8 * kMostGroups) return run_groups<DT, 16, T>(g, nv, ws, stream);
   if (nv >= 16 * g.a.k) return run_groups<DT, 8, T>(g, nv, ws, stream);
   if (nv >= 8 * g.a.k) return run_groups<DT, 4, T>(g, nv, ws, stream);
   if (nv >= 4 * g.a.k) return run_groups<DT, 2, T>(g, nv, ws, stream);
