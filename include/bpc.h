@@ -384,12 +384,15 @@ bpc_status_t bpc_adaptive_update(const bpc_params_t *params,
  *     the mass of all others as one more word.
  *   - A row of row_weight 0 has loss 0 and a gradient of zeros, its logits are not read.
  *   - A record with n = 0 (or soft_weight 0) gives no soft term, a label outside
- *     [0, vocab) (or labels NULL, or hard_weight 0) no hard term.
+ *     [0, vocab) (or labels NULL, or hard_weight 0) no hard term.  A row with neither has
+ *     loss 0 and a gradient of zeros, whatever its logits are.
  *   - Masked student logits (-inf) have probability and gradient 0; if the teacher
  *     gives such a word (or, with TAIL_REST, a rest that is masked as a whole) mass,
- *     the loss is +inf and the gradient of the listed words still -q_i.
- *   - A NaN or +inf among a row's logits makes that row's loss and gradient NaN.  In a
- *     teacher's row it makes values of its record NaN, and so the student's.
+ *     the loss is +inf and the gradient of the listed words still -q_i.  A label that is
+ *     masked gives the loss +inf, too, and its word -1 in place of softmax - 1.
+ *   - Logits without a softmax (a NaN or +inf among them, or all of them -inf) make the loss
+ *     and the gradient of a row that has either term NaN.  In a teacher's row a NaN or +inf
+ *     makes values of its record NaN, and so the student's soft term.
  * Unlike the gradient path these calls take infinities and NaN as described.  Sums are
  * formed in f32 in a fixed order: the same inputs give the same bits (in rows that start
  * elsewhere in their 128-byte line, or of another number, sums may be formed in another order).

@@ -444,6 +444,7 @@ struct Gradient {
   raw *out;
   Stretch st;
   Slope k;
+  bool none;   // the row has neither term (set by prepare, the same in every thread): its gradient is 0, whatever its logits
   __device__ Gradient(const Args &g, const Row<DT> &row_, uint64_t r, uint32_t v0_, uint32_t v1_)
       : row(row_), out(reinterpret_cast<raw *>(g.a.grad) + uniform_off(r * g.a.grad_stride)), st(row_, v0_, v1_) {}
   // (the gradient may be aligned otherwise than the logits)
@@ -469,14 +470,17 @@ struct Gradient {
   }
   // The slope; listed words' gradients take the place of their logits, the label's that of its own.
   __device__ void prepare(const Args &g, float weight, const Stats &stats, Listed<DT, T> &list) {
-    const float soft = stats.inv_q != 0.0f ? weight * g.a.soft * g.c : 0.0f;
-    const float hard = list.label != list.kNone ? weight * g.a.hard : 0.0f;
+    // (a term that is not there counts nothing: its coefficient is no number in a row without a softmax)
+    const bool soft_term = stats.inv_q != 0.0f && g.a.soft != 0.0f, hard_term = HARD && list.label != list.kNone;
+    none = !soft_term && !hard_term;
+    const float soft = soft_term ? weight * g.a.soft * g.c : 0.0f;
+    const float hard = hard_term ? weight * g.a.hard : 0.0f;
     const float ref = ref_of(stats.m);
     k.c2 = g.c2;
     k.m = ref_of(stats.m_r);
     k.far_ = far(stats.m_r, g.c2, two_sums(HARD));
-    k.soft = soft * stats.c_soft;
-    k.hard = hard * stats.c_hard;
+    k.soft = soft_term ? soft * stats.c_soft : 0.0f;
+    k.hard = hard_term ? hard * stats.c_hard : 0.0f;
     if (list.label != list.kNone) {
       const float d = list.s_label - k.m;
       list.s_label = k.soft * exp2_hw(d * g.c2) + (HARD ? k.hard * exp2_hw(d * kLog2e) : 0.0f) - hard;
@@ -611,6 +615,10 @@ __global__ __launch_bounds__(T, WAVES) void distill_twice_kernel(Args g) {
   Four<DT, T> again;
   again.load(row, grad.st, grad.st.b0);
   grad.prepare(g, weight, st, list);
+  if (grad.none) {
+    grad.zero();
+    return;
+  }
   __syncthreads();   // (every listed logit has been read)
   grad.stream(again);
   grad.edges();
@@ -703,6 +711,10 @@ __global__ __launch_bounds__(T, WAVES) void distill_held_kernel(Args g) {
   };
   const Stats st = finish<DT, HARD, T>(g, list, largest, settle, weight, g.a.loss + r, lds);
   grad.prepare(g, weight, st, list);
+  if (grad.none) {
+    grad.zero();
+    return;
+  }
   if (grad.k.far_) {
     grad.stream(Four<DT, T>{});
   } else {
@@ -820,6 +832,10 @@ __global__ __launch_bounds__(T) void distill_grad_kernel(Args g) {
   const uint32_t lo = v0 * E > row.off ? v0 * E - row.off : 0, hi = v1 * E - row.off < row.vocab ? v1 * E - row.off : row.vocab;
   list.template read<HARD != kNoHard>(g, row, r, lo, hi);
   grad.prepare(g, weight, reinterpret_cast<const Stats *>(g.a.stats)[r], list);
+  if (grad.none) {
+    grad.zero();
+    return;
+  }
   // every thread has read the listed logits of its entries before any is written over
   __syncthreads();
   grad.stream(first);
