@@ -497,7 +497,8 @@ struct Gradient {
     for (int i = 0; i < PER; ++i) {
       if (list.idx[i] == list.kNone) continue;
       const float d = list.s[i] - ref;
-      float x = soft * (exp2_hw(d * g.c2) * stats.inv_z - exp2_hw(list.val[i] * g.c2) * stats.inv_q);
+      // (without a soft term what a record says counts nothing, also where its values are no numbers)
+      float x = soft_term ? soft * (exp2_hw(d * g.c2) * stats.inv_z - exp2_hw(list.val[i] * g.c2) * stats.inv_q) : 0.0f;
       if (HARD && hard != 0.0f) x += hard * (exp2_hw(d * kLog2e) * stats.inv_h - (list.idx[i] == list.label ? 1.0f : 0.0f));
       list.s[i] = x;
     }

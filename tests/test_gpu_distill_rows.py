@@ -49,3 +49,46 @@ def test_rows_without_a_term(bpc, vocab, rows, k, dtype, tail, tau):  # noqa: F8
     check_student(bpc, describe_with(1.0, 0.3), x, records, dtype, 1, 2, None, want_nan=nan(lambda full, hard: full), only=only)
     check_student(bpc, describe_with(0.0, 0.3), x, records, dtype, 1, 1, labels, want_nan=nan(lambda full, hard: hard), only=only, in_place=True)
     check_student(bpc, describe_with(0.0, 0.0), x, records, dtype, 1, 2, labels, only=only)
+
+
+@pytest.mark.parametrize("tail", [0, 1])
+@pytest.mark.parametrize("vocab,rows,k,dtype", FORMS)
+def test_no_soft_term_from_a_record_of_nan(bpc, vocab, rows, k, dtype, tail):  # noqa: F811
+    """soft_weight 0: values of a record that are no numbers (a teacher's NaN or +inf) leave the hard term as it is."""
+    rs = np.random.default_rng(vocab + 7)
+    x, records, labels = case(rs, vocab, rows, k, [])
+    n, idx, _, _, _ = records[0]
+    records[1] = (n, idx, np.full(n, np.nan), np.nan, np.nan)                           # a NaN in the teacher's row
+    records[2] = (n, idx, np.where(np.arange(n) == 1, np.nan, -np.inf), 0.0, np.inf)    # +inf
+    labels[1], labels[2], labels[3] = int(idx[0]), int(idx[1]), -100                    # (listed words; no term at all)
+    records[3] = records[1]
+    d = describe(bpc, vocab, k, tail=tail, temperature=2.0, soft_weight=0.0, hard_weight=0.4)
+    check_student(bpc, d, x, records, dtype, 1, 1, labels, only=range(6), in_place=True)
+
+
+def test_gradient_of_the_hard_term_alone(bpc):  # noqa: F811
+    """bpc_distill_grad with soft_weight 0 from statistics of both terms: the hard term's gradient, also where the record's
+    values are no numbers."""
+    import torch
+    import distill_ref as ref
+    from test_gpu_distill import fields, host, make_messages, rows_of, workspace
+    rs = np.random.default_rng(17)
+    vocab, k = 1000, 12
+    x, records, labels = case(rs, vocab, 4, k, [])
+    n, idx, _, _, _ = records[0]
+    records[1] = (n, idx, np.full(n, np.nan), np.nan, np.nan)
+    labels[1], labels[3] = int(idx[3]), -100
+    _, view = rows_of(x, "f32", 1)
+    both = describe(bpc, vocab, k, tail=1, temperature=1.7, soft_weight=1.0, hard_weight=0.4)
+    alone = describe(bpc, vocab, k, tail=1, temperature=1.7, soft_weight=0.0, hard_weight=0.4)
+    msg, lab, ws = make_messages(bpc, both, records), torch.tensor(labels, device="cuda"), workspace(bpc, both, 4)
+    loss, stats = torch.zeros(4, device="cuda"), torch.zeros(4, 32, dtype=torch.uint8, device="cuda")
+    grad = torch.full((4, vocab), 7.0, device="cuda")
+    bpc.bpc_distill_loss(both, view, msg, lab, None, loss, stats, ws)
+    bpc.bpc_distill_grad(alone, view, msg, lab, None, stats, grad)
+    count, at, val, rest, _ = fields(bpc, both, msg, 4)
+    for r in range(4):
+        _, want, _, bound = ref.student_row(host(view)[r], int(count[r]), at[r], val[r], rest[r], 1.7, 0.0, 0.4, True, labels[r], 1.0)
+        bad = np.nonzero(~(np.abs(host(grad)[r] - want) <= bound))[0]
+        assert not bad.size, (r, bad[:5])
+    assert np.isnan(float(loss[1])) and np.isfinite(loss[[0, 2, 3]].cpu().numpy()).all()
