@@ -66,6 +66,59 @@ inline Cut cut_rows(uint64_t rows, uint32_t vocab, int dtype, uint64_t row_strid
 // vectors, and a bit a logit in the 32 KB that these take.
 constexpr uint32_t kMostGroups = 4096, kGroupVecs = 16 * kMostGroups, kGroupWords = 64 * kMostGroups;
 
+// The teacher's call: which form it takes, a workgroup a row, and what that needs.
+enum class TopkForm {
+  any,     // radix select
+  dense,   // the whole row in LDS
+  groups   // by largest logits and sums of groups
+};
+struct TopkPlan {
+  TopkForm form;
+  uint32_t threads;    // of a row's workgroup
+  uint32_t lds;        // dynamic LDS of it, bytes
+  uint32_t lanes;      // groups: neighbouring vectors of a group,
+  uint32_t n_groups;   // ... groups of a row (of whole loads: four vectors a thread),
+  uint32_t cap;        // ... candidates there is room for,
+  uint32_t region;     // ... bytes of LDS for the groups' keys and sums, later the indices level with the k-th, then a bit a
+                       // logit (in whole quads of words a thread)
+  bool few;            // groups: by workgroups for every compute unit, in a launch of their own,
+  size_t ws;           // ... through this much workspace
+};
+constexpr uint32_t kTopThreads = 256;     // of dense rows, of rows by the radix select, of the launch for few rows' groups
+constexpr uint32_t kDenseVocab = 15360;   // most logits of a row in LDS (60 KB)
+inline TopkPlan topk_plan(uint64_t rows, uint32_t vocab, uint32_t k, int dtype, uint64_t row_stride) {
+  const uint32_t nv = row_vecs(vocab, dtype, row_stride), e = 16 / elem_bytes(dtype);
+  TopkPlan p{};
+  p.threads = kTopThreads;
+  if (nv > kGroupVecs || nv * e > kGroupWords) {
+    p.form = TopkForm::any;
+    return p;
+  }
+  if (nv < 2 * k && vocab <= kDenseVocab) {
+    p.form = TopkForm::dense;
+    p.lds = 4 * nv * e;
+    return p;
+  }
+  p.form = TopkForm::groups;
+  // What follows the pass over a row costs every wave about the same, so short rows of few entries take one wave, where
+  // there are rows enough (64 / 256 threads: 16000 x 9000 bf16, k = 20, 90 / 149 us; 4096 x 30522 f16 65 / 74; f32 128 /
+  // 98; k = 300 191 / 120).  Others take 256 threads where they fill the device (512: 119 us for 98 of 4096 x 50257
+  // bf16), and 1024 where they do not (one row of 50,257 f32 20 us with 256).
+  p.threads = nv <= 512 || (rows >= 512 && nv + 8 * k <= 4096) ? 64 : rows >= 512 ? 256 : 1024;
+  // The largest groups of which there are still two or more for each entry (then some 1.4 candidates an entry pass);
+  // never more than kMostGroups.
+  p.lanes = nv > 8 * kMostGroups ? 16 : nv >= 16 * k ? 8 : nv >= 8 * k ? 4 : nv >= 4 * k ? 2 : 1;
+  p.n_groups = (uint32_t)cdiv(nv, 4 * p.threads) * 4 * p.threads / p.lanes;
+  p.cap = 2 * (uint32_t)ru4(k) + 256;
+  const uint32_t words = (uint32_t)cdiv((uint64_t)nv * e, 128 * p.threads) * 4 * p.threads;
+  p.region = 8 * p.n_groups > 4 * words ? 8 * p.n_groups : 4 * words;
+  if (p.region < 4 * p.cap) p.region = 4 * p.cap;
+  p.lds = p.region + 8 * p.cap + 2 * p.n_groups;
+  p.few = rows <= kFewRows && nv >= kLongVecs;
+  p.ws = p.few ? (size_t)rows * p.n_groups * 8 : 0;
+  return p;
+}
+
 constexpr uint32_t kPartialFloats = 4;   // what a chunk hands on: largest logit, sums at both temperatures
 constexpr uint32_t kStatsFloats = BPC_DISTILL_STATS_BYTES / 4;
 

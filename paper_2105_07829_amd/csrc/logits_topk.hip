@@ -217,8 +217,6 @@ struct Tally {
   }
 };
 
-constexpr int kTopThreads = 256;
-
 // Largest logits and sums of exponentials of the groups of four vectors a thread, from vector v of the row on.
 template <int DT, int LANES, int T>
 __device__ void group_sums(const Row<DT> &row, const Stretch &all, uint32_t v, float c2, float (&m)[4], float (&s)[4]) {
@@ -542,8 +540,6 @@ __global__ __launch_bounds__(T) void logits_topk_groups_kernel(TeacherArgs g, ui
 
 // ---- short rows of which many logits are listed: the whole row in LDS
 
-constexpr uint32_t kDenseVocab = 15360;   // (60 KB)
-
 template <int DT>
 __global__ __launch_bounds__(kTopThreads) void logits_topk_dense_kernel(TeacherArgs g) {
   using K = Key<DT>;
@@ -650,57 +646,45 @@ __global__ __launch_bounds__(kTopThreads) void logits_topk_any_kernel(TeacherArg
 }
 
 template <int DT, int LANES, int T>
-static hipError_t run_groups(const TeacherArgs &g, uint32_t nv, uint8_t *ws, hipStream_t stream) {
-  const uint32_t n_groups = (uint32_t)cdiv(nv, 4 * T) * 4 * T / LANES;   // (of whole loads)
-  const uint32_t cap = 2 * (uint32_t)ru4(g.a.k) + 256;
-  // the groups' keys and sums, later the indices level with the k-th, then a bit a logit (in whole quads of words a
-  // thread)
-  const uint32_t words = (uint32_t)cdiv((uint64_t)nv * Num<DT>::E, 128 * T) * 4 * T;
-  uint32_t region = 8 * n_groups > 4 * words ? 8 * n_groups : 4 * words;
-  if (region < 4 * cap) region = 4 * cap;
-  const uint32_t dyn = region + 8 * cap + 2 * n_groups;
+static hipError_t run_groups(const TeacherArgs &g, const TopkPlan &p, uint8_t *ws, hipStream_t stream) {
   float *groups = nullptr;
-  if (g.a.rows <= kFewRows && nv >= kLongVecs) {
-    // few long rows: their groups by workgroups for every compute unit, in a launch of their own
-    groups = reinterpret_cast<float *>(ws);
-    const uint32_t per = 4 * kTopThreads;
-    logits_groups_kernel<DT, LANES><<<dim3(n_groups * LANES / per, (uint32_t)g.a.rows), kTopThreads, 0, stream>>>(g, n_groups, groups);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
+  if constexpr (T == 1024 && LANES > 1) {   // (few rows are long: 1024 threads, four vectors or more for each entry)
+    if (p.few) {
+      groups = reinterpret_cast<float *>(ws);
+      const uint32_t per = 4 * kTopThreads;
+      logits_groups_kernel<DT, LANES><<<dim3(p.n_groups * LANES / per, (uint32_t)g.a.rows), kTopThreads, 0, stream>>>(g, p.n_groups, groups);
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
   }
-  logits_topk_groups_kernel<DT, LANES, T><<<(uint32_t)g.a.rows, T, dyn, stream>>>(g, n_groups, cap, region, groups);
+  logits_topk_groups_kernel<DT, LANES, T><<<(uint32_t)g.a.rows, T, p.lds, stream>>>(g, p.n_groups, p.cap, p.region, groups);
   return hipGetLastError();
 }
 
-// The largest groups of which there are still two or more for each entry (then some 1.4 candidates an entry pass);
-// never more than 4096.
 template <int DT, int T>
-static hipError_t run_lanes(const TeacherArgs &g, uint32_t nv, uint8_t *ws, hipStream_t stream) {
+static hipError_t run_lanes(const TeacherArgs &g, const TopkPlan &p, uint8_t *ws, hipStream_t stream) {
   if constexpr (T != 64)   // (one wave takes short rows only)
-    if (nv > 8 * kMostGroups) return run_groups<DT, 16, T>(g, nv, ws, stream);
-  if (nv >= 16 * g.a.k) return run_groups<DT, 8, T>(g, nv, ws, stream);
-  if (nv >= 8 * g.a.k) return run_groups<DT, 4, T>(g, nv, ws, stream);
-  if (nv >= 4 * g.a.k) return run_groups<DT, 2, T>(g, nv, ws, stream);
-  return run_groups<DT, 1, T>(g, nv, ws, stream);
+    if (p.lanes == 16) return run_groups<DT, 16, T>(g, p, ws, stream);
+  if (p.lanes == 8) return run_groups<DT, 8, T>(g, p, ws, stream);
+  if (p.lanes == 4) return run_groups<DT, 4, T>(g, p, ws, stream);
+  if (p.lanes == 2) return run_groups<DT, 2, T>(g, p, ws, stream);
+  return run_groups<DT, 1, T>(g, p, ws, stream);
 }
 
 template <int DT>
 static hipError_t run_typed(const TeacherArgs &g, uint8_t *ws, hipStream_t stream) {
-  const uint32_t nv = row_vecs(g.a.vocab, DT, g.a.row_stride), k = g.a.k;
-  if (nv > kGroupVecs || nv * Num<DT>::E > kGroupWords) {
+  const TopkPlan p = topk_plan(g.a.rows, g.a.vocab, g.a.k, DT, g.a.row_stride);
+  if (p.form == TopkForm::any) {
     logits_topk_any_kernel<DT><<<(uint32_t)g.a.rows, kTopThreads, 0, stream>>>(g);
     return hipGetLastError();
   }
-  if (nv < 2 * k && g.a.vocab <= kDenseVocab) {
-    logits_topk_dense_kernel<DT><<<(uint32_t)g.a.rows, kTopThreads, 4 * nv * Num<DT>::E, stream>>>(g);
+  if (p.form == TopkForm::dense) {
+    logits_topk_dense_kernel<DT><<<(uint32_t)g.a.rows, kTopThreads, p.lds, stream>>>(g);
     return hipGetLastError();
   }
-  // What follows the pass over a row costs every wave about the same, so short rows of few entries take one wave, where
-  // there are rows enough (64 / 256 threads: 16000 x 9000 bf16, k = 20, 90 / 149 us; 4096 x 30522 f16 65 / 74; f32 128 /
-  // 98; k = 300 191 / 120).  Others take 256 threads where they fill the device (512: 119 us for 98 of 4096 x 50257
-  // bf16), and 1024 where they do not (one row of 50,257 f32 20 us with 256).
-  if (nv <= 512 || (g.a.rows >= 512 && nv + 8 * k <= 4096)) return run_lanes<DT, 64>(g, nv, ws, stream);
-  return g.a.rows >= 512 ? run_lanes<DT, 256>(g, nv, ws, stream) : run_lanes<DT, 1024>(g, nv, ws, stream);
+  return p.threads == 64 ? run_lanes<DT, 64>(g, p, ws, stream)
+         : p.threads == 256 ? run_lanes<DT, 256>(g, p, ws, stream)
+                            : run_lanes<DT, 1024>(g, p, ws, stream);
 }
 
 hipError_t logits_topk(const DistillCall &call, uint8_t *out, uint8_t *ws, hipStream_t stream) {

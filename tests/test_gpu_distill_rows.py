@@ -92,3 +92,27 @@ def test_gradient_of_the_hard_term_alone(bpc):  # noqa: F811
         bad = np.nonzero(~(np.abs(host(grad)[r] - want) <= bound))[0]
         assert not bad.size, (r, bad[:5])
     assert np.isnan(float(loss[1])) and np.isfinite(loss[[0, 2, 3]].cpu().numpy()).all()
+
+
+@pytest.mark.parametrize("rows,vocab,k,dtype", [(1, 131072, 40, "f32"), (32, 131072, 40, "f32"), (3, 262144, 1024, "bf16"), (32, 32768, 700, "f16"),
+                                                (2, 65536, 1000, "f32"), (5, 140001, 300, "f16"), (33, 270001, 20, "f32"), (300, 2000, 16, "bf16")])
+def test_nothing_is_written_behind_the_workspace(bpc, rows, vocab, k, dtype):  # noqa: F811
+    """Every call on a workspace of exactly the bytes that the sizing call answers, between guards."""
+    import torch
+    from test_gpu_distill import tdtype
+    g = torch.Generator(device="cuda").manual_seed(vocab + rows)
+    logits = torch.randn(rows, vocab, generator=g, device="cuda").to(tdtype(dtype))
+    d = bpc.make_distill(bpc.TOPK, vocab, k, temperature=2.0, hard_weight=0.2, tail=bpc.TAIL_REST)
+    size, edge = bpc.distill_workspace_bytes(d, rows), 4096
+    buf = torch.full((size + 2 * edge,), 0x5A, dtype=torch.uint8, device="cuda")
+    ws = buf[edge:edge + size]
+    msg = torch.zeros(bpc.logits_message_bytes(d, rows), dtype=torch.uint8, device="cuda")
+    lab = torch.arange(rows, device="cuda")
+    loss, grad = torch.zeros(rows, device="cuda"), torch.empty_like(logits)
+    print("guards", rows, vocab, k, dtype, size, flush=True)
+    bpc.bpc_logits_topk(d, logits, None, msg, ws)
+    bpc.bpc_distill_loss(d, logits, msg, lab, None, loss, None, ws)
+    bpc.bpc_distill_step(d, logits, msg, lab, None, loss, grad, ws)
+    torch.cuda.synchronize()
+    assert bool((buf[:edge] == 0x5A).all()) and bool((buf[edge + size:] == 0x5A).all())
+    assert bool(torch.isfinite(loss).all())
