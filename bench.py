@@ -264,17 +264,24 @@ def stream_probe(torch, bpc, D):
     return out
 
 
-def sources_digest():
-    """sha256 over the kernel sources: the profile summaries record the digest they were measured
-    at, so a stored traffic figure can be told from one that predates a change to a kernel."""
+def sources_digest(files=None, csrc=os.path.join(ROOT, "paper_2105_07829_amd", "csrc")):
+    """sha256 over kernel sources, `files` and what they include (None: all of them): the profile
+    summaries name the files that the kernels they measured are compiled from and the digest of
+    these at the time, so a stored traffic figure can be told from one that predates a change."""
     import hashlib
+    import re
 
+    todo = list(files) if files else sorted(f for f in os.listdir(csrc) if f.endswith((".hip", ".hpp")))
+    seen = {}
+    while todo:
+        f = todo.pop()
+        if f not in seen:
+            seen[f] = open(os.path.join(csrc, f), "rb").read()
+            todo += [i for i in re.findall(r'^#include "([^"/]+)"', seen[f].decode(), re.M)]
     h = hashlib.sha256()
-    csrc = os.path.join(ROOT, "paper_2105_07829_amd", "csrc")
-    for f in sorted(os.listdir(csrc)):
-        if f.endswith((".hip", ".hpp")):
-            h.update(f.encode())
-            h.update(open(os.path.join(csrc, f), "rb").read())
+    for f in sorted(seen):
+        h.update(f.encode())
+        h.update(seen[f])
     return h.hexdigest()[:16]
 
 
@@ -338,21 +345,21 @@ def cpu_baseline(name, w, n_parts, n_steps, synth, threads=None):
 
 def recorded_traffic(workload, stage):
     """(HBM bytes per launch of a stage as measured with rocprofv3 counters and recorded under
-    profiles/, digest of the kernel sources it was measured at), or (None, None)."""
+    profiles/, digest of the kernel sources it was measured at, those sources), or three times None."""
     names = {"bert_large": "bench_bert_large_dither.txt", "resnet50": "bench_resnet50_topk.txt",
              "vgg16": "bench_vgg16_randk.txt", "bert_base": "bench_bert_base_sign.txt"}
     path = os.path.join(ROOT, "profiles", names.get(workload, f"bench_{workload}.txt"))
-    total, digest = None, None
+    total, digest, files = None, None, None
     try:
         for line in open(path):
             f = line.split()
             if len(f) >= 9 and f[0] == "TRAFFIC" and f[1] == workload and f[2] == stage:
                 total = float(f[f.index("total_bytes") + 1])
             if len(f) >= 2 and f[0] == "SOURCES":
-                digest = f[1]
+                digest, files = f[1], [x for x in f[2:] if x.endswith((".hip", ".hpp"))]
     except OSError:
         pass
-    return total, digest
+    return total, digest, files
 
 
 def main():
@@ -384,10 +391,11 @@ def main():
     alg = algorithmic_bytes_per_elem(w)[dom]
     ach = head["stages"][dom]["algorithmic_GBps"]
     call = {"W": "bpc_compress", "S": "bpc_server_aggregate", "U": "bpc_adaptive_update"}[dom]
-    traffic, traffic_digest = recorded_traffic(args.workload, dom)
-    if traffic is not None and traffic_digest != sources_digest():
+    traffic, traffic_digest, traffic_files = recorded_traffic(args.workload, dom)
+    sources = sources_digest(traffic_files)
+    if traffic is not None and traffic_digest != sources:
         print(f"bench.py: the traffic figure under profiles/ was measured at kernel sources {traffic_digest}, "
-              f"these are {sources_digest()}", file=sys.stderr)
+              f"these are {sources}", file=sys.stderr)
     result = {
         "metric": "GB/s of gradient compressed+EF+decompressed, % of HBM peak, per compressor",
         "value": head["value_GBps"], "unit": "GB/s", "n_gpus": 1, "steps": args.steps, "warmup": args.warmup,
@@ -398,7 +406,7 @@ def main():
                    "error_feedback": "two-way", "update": "adam-style"},
         "roofline": {"bound": "hbm", "achieved": ach, "peak": HBM_PEAK_GBPS, "unit": "GB/s",
                      "frac": round(ach / HBM_PEAK_GBPS, 4), "traffic": traffic,
-                     "traffic_measured_at_sources": traffic_digest, "sources": sources_digest(),
+                     "traffic_measured_at_sources": traffic_digest, "sources": sources,
                      "kernel": f"{call} ({w['kind']})", "algorithmic_bytes_per_element": alg,
                      "elements_per_launch": w["D"]},
         "stages": head["stages"],

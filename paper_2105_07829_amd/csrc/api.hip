@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 #include <mutex>
 #include "cluster.hpp"
+#include "distill_call.hpp"
 #include "distill_geometry.hpp"
 #include "kernels.hpp"
 

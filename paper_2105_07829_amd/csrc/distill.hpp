@@ -1,6 +1,6 @@
 // Rows of logits: how a row is cut into 16-byte vectors and chunks, number types, workgroup
 // reductions.  Shared by the teacher's top-k messages (logits_topk.hip) and the student's loss and
-// gradient (distill.hip).
+// gradient (distill_student.hpp).
 #pragma once
 #include "device_utils.hpp"
 #include "distill_geometry.hpp"

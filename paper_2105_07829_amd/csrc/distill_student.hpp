@@ -21,7 +21,7 @@
 // time); listed logits and gradients passed through a table in LDS instead of a gather and a scatter (1178).
 #pragma once
 #include "distill.hpp"
-#include "kernels.hpp"
+#include "distill_call.hpp"
 
 namespace bpc {
 

@@ -12,7 +12,7 @@
 // it (bisections, second look, index order): 8192 x 131072 bf16, k = 256, 447 us (95 % busy; the pass alone 346 us, 6.2
 // TB/s), 4096 x 50257, k = 64, 97 us (83 %; the pass 63).
 #include "distill.hpp"
-#include "kernels.hpp"
+#include "distill_call.hpp"
 
 namespace bpc {
 
