@@ -398,6 +398,10 @@ bpc_status_t bpc_adaptive_update(const bpc_params_t *params,
  * elsewhere in their 128-byte line, or of another number, sums may be formed in another order).
  * Limits (BPC_ERR_UNSUPPORTED beyond): vocab <= 2^24, k <= BPC_LOGITS_MAX_K (k may exceed
  * vocab), rows < 2^22.  rows == 0 is a no-op returning BPC_OK.
+ * Time: bpc_logits_topk() takes rows of more than 2^18 logits (counted in whole vectors of 16
+ * bytes from the first that a row may start in) and rows in which far more than k logits are level
+ * with the k-th by a radix select: 4096 rows of 262,080 bf16 logits 0.46 ms, of 262,208 3.6 ms;
+ * 4096 equal rows of 50,257 3.1 ms for 0.11.
  */
 #define BPC_LOGITS_MAX_K 1024
 #define BPC_DISTILL_STATS_BYTES 32
@@ -464,9 +468,9 @@ bpc_status_t bpc_distill_grad(const bpc_distill_t *d, const void *logits, bpc_dt
                               void *grad, uint64_t grad_stride, void *hip_stream);
 
 /*
- * Student: loss and gradient in one call; the logits are read once where a compute unit
- * can hold two rows or more, and again while they are in the last-level cache
- * elsewhere.  Arguments as above.
+ * Student: loss and gradient in one call; the logits are read once where a row stays in
+ * registers (rows of up to 32 KB, of up to 128 KB in calls of 512 rows or more), and again
+ * while they are in the last-level cache elsewhere.  Arguments as above.
  */
 bpc_status_t bpc_distill_step(const bpc_distill_t *d, const void *logits, bpc_dtype_t dtype,
                               uint64_t row_stride, uint64_t rows, const void *messages,

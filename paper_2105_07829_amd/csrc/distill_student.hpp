@@ -79,7 +79,10 @@ struct Marks {
 
 // The hard term of a call, which is at temperature 1: none; at the soft one's temperature; at its own; or at its own
 // where that of the soft one is 2 or 4, so that its exponentials are the second and fourth powers of the soft one's
-// (a product or two instead of a multiply-add and an exponential).
+// (a product or two instead of a multiply-add and an exponential).  Powers / own, us: loss and gradient in one call of
+// 2048 x 30522 f16 at temperature 2 55.3 / 61.0, at 4 57.7 / 61.0; of 4096 x 50257 bf16 178 / 183, without the rest 175 /
+// 173; of 1024 x 32000 f32 48.6 / 49.8.  The loss of 4096 x 50257 bf16 81 / 89, without the rest 84 to 88 / 82; the
+// gradient of 2048 x 30522 f16 48.6 / 60.2.
 enum Hard { kNoHard, kSameHard, kOwnHard, kSquareHard, kFourthHard };
 constexpr bool two_sums(int hard) { return hard >= kOwnHard; }
 // 2^(x log2e - ref1) from e = 2^(x c2 - ref2) (ref1 = 2 ref2 or 4 ref2 where that is what it takes).
@@ -857,7 +860,8 @@ static hipError_t run_typed(Args g, DistillRole role, uint8_t *ws, hipStream_t s
   const uint32_t marks_lds = g.a.rest_too ? (uint32_t)cdiv((uint64_t)nv * Num<DT>::E, 32) * 4 : 0;
   if (role == DistillRole::loss && cut.chunks == 1) {
     // (4096 x 50257 bf16 with 256 / 512 / 1024 threads: 68 / 77 / 153 us, what a row costs beside its logits is the same
-    // for each; fewer rows than fill the device take as many threads as there are)
+    // for each.  Fewer rows take 1024; a compute unit has room for one such workgroup, so that more than 256 rows go in two
+    // rounds: 256 / 257 / 511 / 512 rows of 50257 bf16 9.3 / 15.8 / 17.9 / 15.6 us)
     if (nv <= 1024 && g.a.k <= kOneWaveK) distill_loss_kernel<DT, HARD, 64><<<rows, 64, marks_lds, stream>>>(g);
     else if (rows >= 512) distill_loss_kernel<DT, HARD, 256><<<rows, 256, marks_lds, stream>>>(g);
     else distill_loss_kernel<DT, HARD, 1024><<<rows, 1024, marks_lds, stream>>>(g);
@@ -867,7 +871,10 @@ static hipError_t run_typed(Args g, DistillRole role, uint8_t *ws, hipStream_t s
     // Held where two rows or more fit the registers of a compute unit and there are rows enough: 4096 x 50257 bf16 176 us
     // held and 199 in two passes, 2048 x 30522 f16 56 and 80, 2000 x 32000 f32 97 and 119.  One row at a time leaves
     // the memory idle while its sums are joined: 8192 x 131072 bf16 1023 held, 951 in two passes (three rows at a
-    // time).  Few rows: 100 x 30000 bf16 12.9 and 11.0, 61 x 128000 23.2 and 20.5.
+    // time).  Few rows: 100 x 30000 bf16 12.9 and 11.0, 61 x 128000 23.2 and 20.5; 256 / 257 / 511 / 512 rows of 50257 bf16
+    // 14.7 / 22.8 / 30.1 / 23.3 (two rounds of 1024 threads, then held).  The bound of 512 x 6 holds two passes to 80
+    // registers, chosen on bf16, which spills none (own temperature: one); f16 spills 7 to 31: 1024 x 131072 bf16 128 us,
+    // f16 135; with hard labels at temperature 2 131 and 150.
     if (nv <= 512 && g.a.k <= kOneWaveK) return held_rows<DT, HARD, 64, 8, 4>(g, stream);
     if (nv <= 2048) return held_rows<DT, HARD, 256, 8, 5>(g, stream);
     if (nv <= 4096 && rows >= 512) return held_rows<DT, HARD, 256, 16, 4>(g, stream);

@@ -8,6 +8,10 @@
 // through a radix select, which is right for every row.  Of the logits level with the k-th the first ones are listed.
 // The mass of the rest is summed over the unlisted logits, never formed as a difference.
 //
+// The radix select also takes every row past 2^18 logits, for which the bits of the index order and the groups' keys have no
+// room: 4096 x 262080 bf16, k = 64, 462 us and 4096 x 262208 3614; one such row 15 and 681.  4096 x 50257 bf16 with all
+// logits equal, or with fewer than k that are not the type's lowest value, take 3055 and 2919 us for 112.
+//
 // What bounds it: vector issue.  A logit takes 6 to 7 instructions in the pass and about as much again for what follows
 // it (bisections, second look, index order): 8192 x 131072 bf16, k = 256, 447 us (95 % busy; the pass alone 346 us, 6.2
 // TB/s), 4096 x 50257, k = 64, 97 us (83 %; the pass 63).
